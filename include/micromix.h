@@ -25,6 +25,14 @@
  *   mm_calibrate        offline choice of sigma and the split from
  *                       calibration activations (Sec. 3.1 "Offline channel
  *                       assignment strategy"; Def. 1; Appendix C.2 "Derivations")
+ * and for models whose layers hold several experts, each row routed to some of
+ * them (the paper's mixture-of-experts model, Table "tab:moe"):
+ *   mm_group_rows       the rows in order of their experts, on the device
+ *   mm_quantize_act_grouped  mm_quantize_act of the rows in that order, each
+ *                       expert's rows with its own sigma if wanted
+ *   mm_gemm_grouped     mm_gemm of each expert's rows with its weight
+ *   mm_gemv             a few bf16 rows (single tokens), not quantised, times
+ *                       one weight or each row's expert's weight
  *
  * Conventions shared by every call
  * --------------------------------
@@ -106,8 +114,8 @@ typedef enum {
   MM_ERR_ALIGN = 4,  /* a pointer or leading dimension is misaligned        */
   MM_ERR_FORMAT = 5, /* unknown element format, or a and w formats differ   */
   MM_ERR_DEVICE = 6, /* the HIP runtime reported an error at launch         */
-  MM_ERR_WORKSPACE = 7, /* mm_calibrate: workspace smaller than required    */
-  MM_ERR_VALUE = 8      /* a scalar argument out of range (eps)              */
+  MM_ERR_WORKSPACE = 7, /* workspace smaller than required                  */
+  MM_ERR_VALUE = 8      /* a scalar argument out of range (eps, top_k)       */
 } mm_status;
 
 typedef struct {
@@ -276,6 +284,127 @@ mm_status mm_calibrate(const void* x_bf16, int64_t rows, int64_t K, int64_t ldx,
  */
 mm_status mm_calibrate_no_alloc(const void* x_bf16, int64_t rows, int64_t K, int64_t ldx, mm_formats formats,
                                 int32_t* perm_out, int32_t* split_out, void* stream);
+
+/*
+ * Rows grouped by expert
+ * ----------------------
+ * A "slot" is one (token, choice) pair: with top_k choices per token, slot s is
+ * choice s % top_k of token s / top_k, and ids[s] names its expert.  A slot whose
+ * id is outside [0, experts) is in no group (a padded token, or an expert that
+ * another GPU holds): nothing is computed for it.
+ * A row-group map places the slots in "packed rows", expert by expert, ascending
+ * inside an expert, each expert's first row a multiple of 32 (a row group of the
+ * packed layout):
+ *   c_e = number of slots of expert e
+ *   starts[0] = 0, starts[e + 1] = starts[e] + 32 ceil(c_e / 32)
+ *   slots[starts[e] + i] = the i-th slot of expert e, i < c_e; -1 for every
+ *                   other packed row below the capacity
+ *   owners[g]       expert of row group g (packed rows 32 g .. 32 g + 31), -1
+ *                   from starts[experts] / 32 on
+ * Its capacity is 32 floor((rows + 31 min(experts, rows)) / 32), enough for every
+ * choice of ids.  The map is one int32 device buffer: starts at word 0, slots and
+ * owners at the word offsets that mm_group_layout_sizes() gives, behind them
+ * lists that the grouped calls use.
+ */
+typedef struct {
+  int64_t rows;    /* slots, 1 .. 2^26                                     */
+  int64_t experts; /* 1 .. 1024                                            */
+  int32_t* map;    /* device, 16-byte aligned                              */
+} mm_row_groups;
+
+typedef struct {
+  int64_t capacity; /* packed rows                        */
+  int64_t slots;    /* word offset of slots [capacity]       */
+  int64_t owners;   /* word offset of owners [capacity / 32] */
+  int64_t bytes;    /* of the whole map                     */
+} mm_group_sizes;
+
+/*
+ * Sizes of a row-group map.  Host-only arithmetic.  Errors: MM_ERR_NULL (out is
+ * NULL), MM_ERR_SHAPE.
+ */
+mm_status mm_group_layout_sizes(int64_t rows, int64_t experts, mm_group_sizes* out);
+
+/*
+ * Fill out's map from the experts of its slots.  The result depends on the ids
+ * only (the order inside an expert is the slots').
+ *   ids     device, int32 [out->rows], 4-byte aligned, any values.
+ * One launch up to 4096 slots, two above.  Errors: MM_ERR_NULL, MM_ERR_SHAPE,
+ * MM_ERR_ALIGN, MM_ERR_DEVICE.
+ */
+mm_status mm_group_rows(const int32_t* ids, const mm_row_groups* out, void* stream);
+
+/*
+ * mm_quantize_act of the slots' rows: packed row p with slot s = slots[p] takes row
+ * s / top_k of x, its channels gathered by its expert's sigma.  Codes and scales
+ * are bit for bit those of mm_quantize_act on that row.  Packed rows without a
+ * slot are neither read nor written (mm_gemm_grouped uses them for nothing).
+ *   x_bf16   device, bf16 [ceil(groups->rows / top_k), K] row-major, row stride
+ *            ldx elements (ldx >= K, ldx % 8 == 0, 16-byte aligned), finite.
+ *   top_k    slots per row of x, 1 .. 2^26 (MM_ERR_VALUE otherwise): a token's choices
+ *            share its row (the experts' first layers), or 1 where every slot has
+ *            a row of its own (their second).
+ *   perm     device, int32, 16-byte aligned: sigma of expert e at perm + e *
+ *            perm_stride, perm_stride 0 (one sigma for all experts) or at least K
+ *            and a multiple of 4.
+ *   groups   a map that mm_group_rows filled, on this stream or before it.
+ *   out      descriptor with rows = the map's capacity.
+ * K may be at most 32768.  Errors: those of mm_quantize_act, MM_ERR_VALUE.
+ */
+mm_status mm_quantize_act_grouped(const void* x_bf16, int64_t ldx, int64_t top_k, const int32_t* perm,
+                                  int64_t perm_stride, const mm_row_groups* groups, const mm_mx_tensor* out,
+                                  void* stream);
+
+/*
+ * mm_gemm of each expert's packed rows with its weight, results in slot order:
+ *   Y[s, n] = the Y of mm_gemm for packed row p (slots[p] = s) and row n of the
+ *             weight of expert ids[s]
+ * up to the order of the fp32 sums.  Rows of Y whose slot is in no group are left as
+ * they were.
+ *   a       the packed rows (rows = the map's capacity).
+ *   w       descriptor of ONE expert's weight (rows = N, same K, split and formats as
+ *           a).  Each of its buffers holds groups->experts such weights one after
+ *           the other, every mm_mx_layout_sizes() bytes.
+ *   y_bf16  device, bf16 [groups->rows, N] row-major, row stride ldy elements
+ *           (ldy >= N, ldy % 8 == 0, 16-byte aligned).
+ * The launch depends on the sizes only, so it can be captured and replayed with
+ * other ids.  Errors: those of mm_gemm.
+ */
+mm_status mm_gemm_grouped(const mm_mx_tensor* a, const mm_mx_tensor* w, const mm_row_groups* groups, void* y_bf16,
+                          int64_t ldy, void* stream);
+
+/*
+ * Device workspace mm_gemv needs for `rows` rows (1 .. 16).  Host-only arithmetic.
+ * Errors: MM_ERR_NULL (bytes is NULL), MM_ERR_SHAPE, MM_ERR_SPLIT.
+ */
+mm_status mm_gemv_workspace_size(int64_t rows, int64_t K, mm_split split, int64_t* bytes);
+
+/*
+ * A few rows of bf16 activations, not quantised, times quantised weights:
+ *   Y[r, n] = bf16( sum_j W_e[n, j] x[r / top_k, sigma_e[j]] )
+ * with the weights' exact values, fp32 sums and one rounding to nearest even at the
+ * end; e = ids[r], or 0 without ids.  (A weight below 2^-126 in magnitude may count as
+ * 0.)  Rows whose id is outside [0, experts) are left as they were.
+ *   x_bf16      device, bf16 [ceil(rows / top_k), K], row stride ldx elements (ldx >=
+ *               K; 2-byte aligned), finite.
+ *   rows        rows of Y, 1 .. 16 (more: mm_quantize_act and mm_gemm).
+ *   top_k       1 .. 16, rows of Y per row of x.
+ *   perm, perm_stride  as for mm_quantize_act_grouped.
+ *   w, experts  as for mm_gemm_grouped (experts 1 .. 1024).
+ *   ids         device, int32 [rows], 4-byte aligned, any values; NULL: every row
+ *               takes the first weight.
+ *   workspace   device, caller-owned, 16-byte aligned, at least
+ *               mm_gemv_workspace_size() bytes (NULL where that is 0); contents on
+ *               entry ignored, on exit unspecified.  Calls that overlap in time must
+ *               not share it.
+ *   y_bf16      device, bf16 [rows, N], row stride ldy elements (ldy >= N, ldy % 8 ==
+ *               0, 16-byte aligned).
+ * Errors: MM_ERR_NULL, MM_ERR_SHAPE, MM_ERR_SPLIT, MM_ERR_ALIGN, MM_ERR_FORMAT,
+ * MM_ERR_VALUE (top_k), MM_ERR_WORKSPACE, MM_ERR_DEVICE.
+ */
+mm_status mm_gemv(const void* x_bf16, int64_t ldx, int64_t rows, int64_t top_k, const int32_t* perm,
+                  int64_t perm_stride, const mm_mx_tensor* w, int64_t experts, const int32_t* ids, void* workspace,
+                  int64_t workspace_bytes, void* y_bf16, int64_t ldy, void* stream);
 
 /* Static English name of a status code. */
 const char* mm_status_str(mm_status s);

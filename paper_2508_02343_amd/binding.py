@@ -56,6 +56,15 @@ class MMSizes(ctypes.Structure):
     _fields_ = [("q4", ctypes.c_int64), ("q6", ctypes.c_int64), ("q8", ctypes.c_int64), ("sc", ctypes.c_int64)]
 
 
+class MMRowGroups(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("experts", ctypes.c_int64), ("map", ctypes.c_void_p)]
+
+
+class MMGroupSizes(ctypes.Structure):
+    _fields_ = [("capacity", ctypes.c_int64), ("slots", ctypes.c_int64), ("owners", ctypes.c_int64),
+                ("bytes", ctypes.c_int64)]
+
+
 def _load(path: str = LIB_PATH) -> ctypes.CDLL:
     if not os.path.exists(path):
         raise ImportError(f"{path} is missing: build it first (python -m paper_2508_02343_amd.build_lib)")
@@ -83,6 +92,16 @@ def _load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.mm_calibrate.restype = ctypes.c_int
     lib.mm_calibrate_no_alloc.argtypes = [P, I64, I64, I64, MMFormats, P, P, P]
     lib.mm_calibrate_no_alloc.restype = ctypes.c_int
+    G = ctypes.POINTER(MMRowGroups)
+    lib.mm_group_layout_sizes.argtypes = [I64, I64, ctypes.POINTER(MMGroupSizes)]
+    lib.mm_group_rows.argtypes = [P, G, P]
+    lib.mm_quantize_act_grouped.argtypes = [P, I64, I64, P, I64, G, T, P]
+    lib.mm_gemm_grouped.argtypes = [T, T, G, P, I64, P]
+    lib.mm_gemv_workspace_size.argtypes = [I64, I64, MMSplit, ctypes.POINTER(I64)]
+    lib.mm_gemv.argtypes = [P, I64, I64, I64, P, I64, T, I64, P, P, I64, P, I64, P]
+    for f in (lib.mm_group_layout_sizes, lib.mm_group_rows, lib.mm_quantize_act_grouped, lib.mm_gemm_grouped,
+              lib.mm_gemv_workspace_size, lib.mm_gemv):
+        f.restype = ctypes.c_int
     if lib.mm_abi_version() != ABI_VERSION:
         raise ImportError(f"{path}: ABI version {lib.mm_abi_version()}, this binding needs {ABI_VERSION}")
     return lib
@@ -95,6 +114,8 @@ lib = _load()
 # kernel takes 4 us, and filling a structure took 1 us of each call's time.
 _DESC = struct.Struct("@qqiiiiiPPPP")
 assert _DESC.size == ctypes.sizeof(MMTensor)
+_GROUPS = struct.Struct("@qqP")  # an mm_row_groups
+assert _GROUPS.size == ctypes.sizeof(MMRowGroups)
 
 
 def _load_packed(path: str = LIB_PATH) -> ctypes.CDLL:
@@ -103,7 +124,12 @@ def _load_packed(path: str = LIB_PATH) -> ctypes.CDLL:
     fast.mm_quantize_act.argtypes = fast.mm_quantize_weight.argtypes = [P, I64, P, D, P]
     fast.mm_rmsnorm_quantize_act.argtypes = [P, I64, P, ctypes.c_float, P, D, P]
     fast.mm_gemm.argtypes = [D, D, P, I64, P]
-    for f in (fast.mm_quantize_act, fast.mm_quantize_weight, fast.mm_gemm, fast.mm_rmsnorm_quantize_act):
+    fast.mm_group_rows.argtypes = [P, D, P]
+    fast.mm_quantize_act_grouped.argtypes = [P, I64, I64, P, I64, D, D, P]
+    fast.mm_gemm_grouped.argtypes = [D, D, D, P, I64, P]
+    fast.mm_gemv.argtypes = [P, I64, I64, I64, P, I64, D, I64, P, P, I64, P, I64, P]
+    for f in (fast.mm_quantize_act, fast.mm_quantize_weight, fast.mm_gemm, fast.mm_rmsnorm_quantize_act,
+              fast.mm_group_rows, fast.mm_quantize_act_grouped, fast.mm_gemm_grouped, fast.mm_gemv):
         f.restype = ctypes.c_int
     return fast
 
@@ -306,6 +332,226 @@ def gemm(a: MXTensor, w: MXTensor, y: torch.Tensor | None = None, stream=None) -
           or y.device != device):
         raise ValueError(f"y must be a bfloat16 [{M}, {N}] tensor with unit column stride on {device}")
     _check(_fast.mm_gemm(a._packed(), w._packed(), y.data_ptr(), y.stride(0), _stream_int(stream)))
+    return y
+
+
+# ---- rows grouped by expert ----
+
+
+@functools.lru_cache(maxsize=1024)
+def _group_sizes(rows: int, experts: int) -> tuple:
+    """mm_group_layout_sizes as (capacity, slots, owners, bytes)."""
+    sz = MMGroupSizes()
+    _check(lib.mm_group_layout_sizes(rows, experts, ctypes.byref(sz)))
+    return sz.capacity, sz.slots, sz.owners, sz.bytes
+
+
+@dataclass
+class RowGroups:
+    """Row-group map in device memory (include/micromix.h): `rows` slots in order
+    of their experts.  starts [experts + 1], slots [capacity] and owners
+    [capacity / 32] are views of the one int32 buffer `map`."""
+
+    rows: int
+    experts: int
+    map: torch.Tensor
+
+    def __post_init__(self):
+        self.capacity, slots, owners, nbytes = _group_sizes(int(self.rows), int(self.experts))
+        m = self.map
+        if m.dtype != torch.int32 or m.dim() != 1 or not m.is_contiguous() or m.nbytes < nbytes:
+            raise ValueError(f"map must be a contiguous int32 tensor of at least {nbytes // 4} words")
+        self.starts = m[:self.experts + 1]
+        self.slots = m[slots:slots + self.capacity]
+        self.owners = m[owners:owners + self.capacity // 32]
+        self.device_index = m.get_device()
+
+    @classmethod
+    def empty(cls, rows: int, experts: int, device="cuda") -> "RowGroups":
+        rows, experts = int(rows), int(experts)
+        return cls(rows, experts, torch.empty(_group_sizes(rows, experts)[3] // 4, dtype=torch.int32, device=device))
+
+    def _packed(self) -> bytes:
+        return _GROUPS.pack(self.rows, self.experts, self.map.data_ptr())
+
+
+@dataclass
+class MXStack:
+    """`count` quantised operands of the same size, one per expert: each of the
+    buffers holds the experts' one after the other.  stack[e] is expert e's, an
+    MXTensor on the same memory (quantize_weight(..., out=stack[e]) fills it)."""
+
+    count: int
+    rows: int
+    K: int
+    split: tuple[int, int, int]
+    q4: torch.Tensor | None
+    q6: torch.Tensor | None
+    q8: torch.Tensor | None
+    sc: torch.Tensor
+    formats: tuple[str, str] = DEFAULT_FORMATS
+
+    @classmethod
+    def empty(cls, count: int, rows: int, K: int, split, device="cuda", formats=DEFAULT_FORMATS) -> "MXStack":
+        if count < 1:
+            raise ValueError("a stack holds at least one operand")
+        split = tuple(map(int, split))
+        bufs = (torch.empty(count * n, dtype=torch.uint8, device=device) if n else None
+                for n in _buffer_sizes(rows, K, split))
+        return cls(count, rows, K, split, *bufs, tuple(formats))
+
+    def __len__(self) -> int:
+        return self.count
+
+    def __getitem__(self, e: int) -> MXTensor:
+        if not -self.count <= e < self.count:
+            raise IndexError(f"expert {e} of {self.count}")
+        e %= self.count
+        bufs = (None if b is None else b[e * n:(e + 1) * n]
+                for b, n in zip((self.q4, self.q6, self.q8, self.sc), _buffer_sizes(self.rows, self.K, self.split)))
+        return MXTensor(self.rows, self.K, self.split, *bufs, self.formats)
+
+    _packed = MXTensor._packed  # the first expert's descriptor
+
+
+def _here(index: int, name: str) -> None:
+    """A tensor's device is the current one (kernels are launched there)."""
+    if index < 0 or index != (torch.cuda.current_device() if _raw_device is None else _raw_device()):
+        raise ValueError(f"{name} must be on the current device")
+
+
+def _check_perms(perm: torch.Tensor, experts: int, K: int, index: int) -> int:
+    """One sigma [K] for all experts, or one each [experts, K]; its stride."""
+    if (perm.dtype != torch.int32 or not perm.is_contiguous() or perm.get_device() != index
+            or (tuple(perm.shape) != (K,) and tuple(perm.shape) != (experts, K))):
+        raise ValueError(f"perm must be a contiguous int32 tensor [{K}] or [{experts}, {K}] on x's device")
+    return 0 if perm.dim() == 1 else K
+
+
+def group_rows(ids: torch.Tensor, experts: int, out: RowGroups | None = None, stream=None) -> RowGroups:
+    """mm_group_rows: the slots whose experts `ids` names (int32, any shape, taken in
+    order) grouped by expert.  Ids outside [0, experts) are in no group."""
+    if ids.dtype != torch.int32 or not ids.is_contiguous():
+        raise ValueError("ids must be a contiguous int32 device tensor")
+    index = ids.get_device()
+    _here(index, "ids")
+    if out is None:
+        out = RowGroups.empty(ids.numel(), experts, device=ids.device)
+    elif out.rows != ids.numel() or out.experts != experts or out.device_index != index:
+        raise ValueError(f"out is for {out.rows} slots of {out.experts} experts, got {ids.numel()} of {experts}")
+    _check(_fast.mm_group_rows(ids.data_ptr(), out._packed(), _stream_int(stream)))
+    return out
+
+
+def quantize_act_grouped(x: torch.Tensor, groups: RowGroups, perm: torch.Tensor, split, top_k: int = 1,
+                         out: MXTensor | None = None, stream=None, formats=DEFAULT_FORMATS) -> MXTensor:
+    """mm_quantize_act_grouped: bf16 rows x [slots / top_k, K] quantised in the order
+    of `groups` (slot s takes row s // top_k), with one sigma [K] or one per expert
+    [experts, K].  The result has groups.capacity rows; those without a slot are
+    not written."""
+    if x.dtype != torch.bfloat16 or x.dim() != 2 or x.stride(1) != 1 or not x.is_cuda:
+        raise ValueError("x must be a 2-D row-major bfloat16 device tensor")
+    rows, K = x.shape
+    index = x.get_device()
+    _here(index, "x")
+    if rows * top_k != groups.rows or groups.device_index != index:
+        raise ValueError(f"x has {rows} rows of {top_k} slots each, the groups are of {groups.rows} slots (on x's device)")
+    stride = _check_perms(perm, groups.experts, K, index)
+    split = tuple(map(int, split))
+    if out is None:
+        out = MXTensor.empty(groups.capacity, K, split, device=x.device, formats=formats)
+    else:
+        _check_layout(out, groups.capacity, K, split, x.device, "out")
+    _check(_fast.mm_quantize_act_grouped(x.data_ptr(), x.stride(0), top_k, perm.data_ptr(), stride,
+                                         groups._packed(), out._packed(), _stream_int(stream)))
+    return out
+
+
+def _check_weights(w, index: int, device) -> int:
+    """An MXTensor, or an MXStack (its buffers hold count operands); the number of experts."""
+    if not isinstance(w, MXStack):
+        _check_buffers(w, w.rows, w.K, tuple(map(int, w.split)), device, "w")
+        return 1
+    for b, buf, need in zip(("q4", "q6", "q8", "sc"), (w.q4, w.q6, w.q8, w.sc), _buffer_sizes(w.rows, w.K, w.split)):
+        n = 0 if buf is None else buf.nbytes
+        if n < need * w.count:
+            raise ValueError(f"w.{b} holds {n} bytes, {w.count} experts need {need * w.count}")
+        if buf is not None and (buf.get_device() != index or not buf.is_contiguous()):
+            raise ValueError(f"w.{b} must be contiguous and on {device}")
+    return w.count
+
+
+def _result(y: torch.Tensor | None, M: int, N: int, index: int, device) -> torch.Tensor:
+    """A bf16 [M, N] result; a new one is zero, as some of its rows may not be written."""
+    if y is None:
+        return torch.zeros((M, _round16(N) if N % 8 else N), dtype=torch.bfloat16, device=device)[:, :N]
+    if (y.dtype != torch.bfloat16 or y.dim() != 2 or tuple(y.shape) != (M, N) or y.stride(1) != 1
+            or y.get_device() != index):
+        raise ValueError(f"y must be a bfloat16 [{M}, {N}] tensor with unit column stride on {device}")
+    return y
+
+
+def gemm_grouped(a: MXTensor, w: MXStack, groups: RowGroups, y: torch.Tensor | None = None,
+                 stream=None) -> torch.Tensor:
+    """mm_gemm_grouped: Y [slots, N], row s the product of slot s's packed row and its
+    expert's weight.  Rows of slots in no group are left as they were in `y` (zero
+    without it)."""
+    device, index = a.sc.device, a.sc.get_device()
+    _here(index, "a")
+    _check_buffers(a, groups.capacity, a.K, tuple(map(int, a.split)), device, "a")
+    if a.rows != groups.capacity or groups.device_index != index:
+        raise ValueError(f"a has {a.rows} rows, the groups' capacity is {groups.capacity} (on a's device)")
+    if not isinstance(w, MXStack) or _check_weights(w, index, device) != groups.experts:
+        raise ValueError(f"w must be an MXStack of the groups' {groups.experts} experts")
+    y = _result(y, groups.rows, w.rows, index, device)
+    _check(_fast.mm_gemm_grouped(a._packed(), w._packed(), groups._packed(), y.data_ptr(), y.stride(0),
+                                 _stream_int(stream)))
+    return y
+
+
+@functools.lru_cache(maxsize=1024)
+def _gemv_workspace(rows: int, K: int, split: tuple) -> int:
+    n = ctypes.c_int64()
+    _check(lib.mm_gemv_workspace_size(rows, K, MMSplit(*split), ctypes.byref(n)))
+    return n.value
+
+
+def gemv_workspace_size(rows: int, K: int, split) -> int:
+    """mm_gemv_workspace_size: device bytes mm_gemv needs."""
+    return _gemv_workspace(int(rows), int(K), tuple(map(int, split)))
+
+
+def gemv(x: torch.Tensor, w: MXTensor | MXStack, perm: torch.Tensor, ids: torch.Tensor | None = None, top_k: int = 1,
+         y: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """mm_gemv: bf16 rows x [rows / top_k, K], not quantised, times the weight w
+    (MXTensor), or, with ids (int32 [rows]) naming each row's expert, times the expert's
+    weight of w (MXStack); at most 16 rows of Y.  perm as for
+    quantize_act_grouped.  Rows whose id names no expert are left as they were in
+    `y` (zero without it)."""
+    if x.dtype != torch.bfloat16 or x.dim() != 2 or x.stride(1) != 1 or not x.is_cuda:
+        raise ValueError("x must be a 2-D row-major bfloat16 device tensor")
+    n, K = x.shape
+    device, index = x.device, x.get_device()
+    _here(index, "x")
+    experts = _check_weights(w, index, device)
+    if w.K != K:
+        raise ValueError(f"x has {K} channels, w {w.K}")
+    if (ids is None) != (not isinstance(w, MXStack)):
+        raise ValueError("ids go with an MXStack, an MXTensor takes none")
+    rows = n * top_k
+    if ids is not None and (ids.dtype != torch.int32 or not ids.is_contiguous() or ids.numel() != rows
+                            or ids.get_device() != index):
+        raise ValueError(f"ids must be a contiguous int32 tensor of {rows} elements on x's device")
+    stride = _check_perms(perm, experts, K, index)
+    need = gemv_workspace_size(rows, K, w.split)
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    elif not workspace.is_contiguous() or workspace.get_device() != index:
+        raise ValueError("workspace must be contiguous and on x's device")
+    y = _result(y, rows, w.rows, index, device)
+    _check(_fast.mm_gemv(x.data_ptr(), x.stride(0), rows, top_k, perm.data_ptr(), stride, w._packed(),
+                         experts, 0 if ids is None else ids.data_ptr(), workspace.data_ptr(), workspace.nbytes,
+                         y.data_ptr(), y.stride(0), _stream_int(stream)))
     return y
 
 

@@ -9,6 +9,7 @@
 
 #include "../../include/micromix.h"
 #include "gemm_route.hpp"
+#include "grouped.hpp"
 #include "kernels.hpp"
 
 namespace {
@@ -175,6 +176,46 @@ mm::Operand operand(const mm_mx_tensor* t) {
   return o;
 }
 
+// bf16 [.., w->rows] results.
+mm_status check_result(const mm_mx_tensor* w, const void* y, int64_t ldy, const char* who) {
+  if (!y) return fail(MM_ERR_NULL, "%s: y is NULL", who);
+  if (ldy < w->rows) return fail(MM_ERR_SHAPE, "%s: ldy=%lld below N=%lld", who, (long long)ldy, (long long)w->rows);
+  if (!aligned16(y) || ldy % 8 != 0) return fail(MM_ERR_ALIGN, "%s: y must be 16-byte aligned with ldy %% 8 == 0", who);
+  return MM_OK;
+}
+
+// Operands and result of a product.
+mm_status check_product(const mm_mx_tensor* a, const mm_mx_tensor* w, const void* y, int64_t ldy, const char* who) {
+  mm_status st = check_tensor(a, "a");
+  if (st != MM_OK) return st;
+  st = check_tensor(w, "w");
+  if (st != MM_OK) return st;
+  if (!y) return fail(MM_ERR_NULL, "%s: y is NULL", who);
+  if (a->K != w->K) return fail(MM_ERR_SHAPE, "%s: K differs (%lld vs %lld)", who, (long long)a->K, (long long)w->K);
+  if (a->split.p4 != w->split.p4 || a->split.p6 != w->split.p6 || a->split.p8 != w->split.p8)
+    return fail(MM_ERR_SHAPE, "%s: a and w must share the split", who);
+  if (format_set(a) != format_set(w)) return fail(MM_ERR_FORMAT, "%s: a and w must share the element formats", who);
+  return check_result(w, y, ldy, who);
+}
+
+mm::GemmArgs gemm_args(const mm_mx_tensor* a, const mm_mx_tensor* w, void* y, int64_t ldy) {
+  mm::GemmArgs g;
+  g.w = operand(w);
+  g.x = operand(a);
+  const Layout l = layout(a->rows, a->split);
+  for (int k = 0; k < 3; ++k) g.steps[k] = l.steps[k];
+  g.y = static_cast<uint16_t*>(y);
+  g.ldy = ldy;
+  g.fs = format_set(a);
+  return g;
+}
+
+mm_status check_gemv_rows(int64_t rows, const char* who) {
+  if (rows <= 0 || rows > mm::kGemvMaxRows)
+    return fail(MM_ERR_SHAPE, "%s: rows=%lld out of range (1 .. %d)", who, (long long)rows, mm::kGemvMaxRows);
+  return MM_OK;
+}
+
 hipError_t launch_gemm(const mm::GemmArgs& g, hipStream_t s) {
   mm::Device dev;
   hipError_t e = mm::current_device(&dev);
@@ -237,25 +278,9 @@ mm_status mm_rmsnorm_quantize_act(const void* x_bf16, int64_t ldx, const void* g
 
 mm_status mm_gemm(const mm_mx_tensor* a, const mm_mx_tensor* w, void* y_bf16, int64_t ldy, void* stream) {
   g_err[0] = 0;
-  mm_status st = check_tensor(a, "a");
+  mm_status st = check_product(a, w, y_bf16, ldy, "mm_gemm");
   if (st != MM_OK) return st;
-  st = check_tensor(w, "w");
-  if (st != MM_OK) return st;
-  if (!y_bf16) return fail(MM_ERR_NULL, "mm_gemm: y is NULL");
-  if (a->K != w->K) return fail(MM_ERR_SHAPE, "mm_gemm: K differs (%lld vs %lld)", (long long)a->K, (long long)w->K);
-  if (a->split.p4 != w->split.p4 || a->split.p6 != w->split.p6 || a->split.p8 != w->split.p8)
-    return fail(MM_ERR_SHAPE, "mm_gemm: a and w must share the split");
-  if (format_set(a) != format_set(w)) return fail(MM_ERR_FORMAT, "mm_gemm: a and w must share the element formats");
-  if (ldy < w->rows) return fail(MM_ERR_SHAPE, "mm_gemm: ldy=%lld below N=%lld", (long long)ldy, (long long)w->rows);
-  if (!aligned16(y_bf16) || ldy % 8 != 0) return fail(MM_ERR_ALIGN, "mm_gemm: y must be 16-byte aligned with ldy %% 8 == 0");
-  mm::GemmArgs g;
-  g.w = operand(w);
-  g.x = operand(a);
-  const Layout l = layout(a->rows, a->split);
-  for (int k = 0; k < 3; ++k) g.steps[k] = l.steps[k];
-  g.y = static_cast<uint16_t*>(y_bf16);
-  g.ldy = ldy;
-  g.fs = format_set(a);
+  const mm::GemmArgs g = gemm_args(a, w, y_bf16, ldy);
   hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t e = launch_gemm(g, s);
   if (e != hipSuccess) return fail(MM_ERR_DEVICE, "mm_gemm: launch failed: %s", hipGetErrorString(e));
@@ -338,6 +363,235 @@ mm_status mm_calibrate_no_alloc(const void* x_bf16, int64_t rows, int64_t K, int
                                 int32_t* perm_out, int32_t* split_out, void* stream) {
   g_err[0] = 0;
   return calibrate(x_bf16, rows, K, ldx, formats, nullptr, 0, perm_out, split_out, stream, "mm_calibrate_no_alloc");
+}
+
+namespace {
+
+mm_status check_group_shape(int64_t rows, int64_t experts, const char* who) {
+  if (rows <= 0 || rows > mm::kMaxGroupedRows)
+    return fail(MM_ERR_SHAPE, "%s: rows=%lld out of range (1 .. 2^26)", who, (long long)rows);
+  if (experts <= 0 || experts > mm::kMaxExperts)
+    return fail(MM_ERR_SHAPE, "%s: experts=%lld out of range (1 .. %lld)", who, (long long)experts,
+                (long long)mm::kMaxExperts);
+  return MM_OK;
+}
+
+mm_status check_groups(const mm_row_groups* g, const char* who) {
+  if (!g) return fail(MM_ERR_NULL, "%s: groups is NULL", who);
+  mm_status st = check_group_shape(g->rows, g->experts, who);
+  if (st != MM_OK) return st;
+  if (!g->map) return fail(MM_ERR_NULL, "%s: the row-group map is NULL", who);
+  if (!aligned16(g->map)) return fail(MM_ERR_ALIGN, "%s: the row-group map must be 16-byte aligned", who);
+  return MM_OK;
+}
+
+mm::RowTile* tile_list(const mm_row_groups* g, const mm::GroupLayout& l, int k) {
+  return reinterpret_cast<mm::RowTile*>(g->map + l.tiles[k]);
+}
+
+// sigma of each expert at perm + e * perm_stride.
+mm_status check_perms(const int32_t* perm, int64_t perm_stride, int64_t K, const char* who) {
+  if (!perm) return fail(MM_ERR_NULL, "%s: perm is NULL", who);
+  if (!aligned16(perm)) return fail(MM_ERR_ALIGN, "%s: perm must be 16-byte aligned", who);
+  if (perm_stride != 0 && perm_stride < K)
+    return fail(MM_ERR_SHAPE, "%s: perm_stride=%lld below K=%lld", who, (long long)perm_stride, (long long)K);
+  if (perm_stride % 4 != 0) return fail(MM_ERR_ALIGN, "%s: perm_stride must be a multiple of 4", who);
+  return MM_OK;
+}
+
+mm::ExpertStride expert_stride(const mm_mx_tensor* w) {
+  const Layout l = layout(w->rows, w->split);
+  return mm::ExpertStride{{l.bytes[0], l.bytes[1], l.bytes[2]}, l.bytes[3]};
+}
+
+}  // namespace
+
+mm_status mm_group_layout_sizes(int64_t rows, int64_t experts, mm_group_sizes* out) {
+  g_err[0] = 0;
+  if (!out) return fail(MM_ERR_NULL, "mm_group_layout_sizes: out is NULL");
+  mm_status st = check_group_shape(rows, experts, "mm_group_layout_sizes");
+  if (st != MM_OK) return st;
+  const mm::GroupLayout l = mm::group_layout(rows, experts);
+  out->capacity = l.capacity;
+  out->slots = l.slots;
+  out->owners = l.owners;
+  out->bytes = l.words * (int64_t)sizeof(int32_t);
+  return MM_OK;
+}
+
+mm_status mm_group_rows(const int32_t* ids, const mm_row_groups* out, void* stream) {
+  g_err[0] = 0;
+  const char* who = "mm_group_rows";
+  if (!ids) return fail(MM_ERR_NULL, "%s: ids is NULL", who);
+  mm_status st = check_groups(out, who);
+  if (st != MM_OK) return st;
+  if ((uintptr_t)ids & 3u) return fail(MM_ERR_ALIGN, "%s: ids must be 4-byte aligned", who);
+  const mm::GroupLayout l = mm::group_layout(out->rows, out->experts);
+  mm::GroupArgs a;
+  a.ids = ids;
+  a.rows = out->rows;
+  a.experts = (int)out->experts;
+  a.starts = out->map;
+  a.slots = out->map + l.slots;
+  a.owners = out->map + l.owners;
+  a.counts = out->map + l.counts;
+  for (int k = 0; k < mm::kTileLists; ++k) {
+    a.tiles[k] = tile_list(out, l, k);
+    a.ntiles[k] = (int)l.ntiles[k];
+  }
+  a.groups = (int)(l.capacity / mm::kRowGroup);
+  a.blocks = (int)l.blocks;
+  a.turns = (int)((out->rows + l.blocks * 1024 - 1) / (l.blocks * 1024));
+  mm::Device dev;
+  hipError_t e = mm::current_device(&dev);
+  if (e == hipSuccess) e = mm::launch_group_rows(a, dev, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return fail(MM_ERR_DEVICE, "%s: launch failed: %s", who, hipGetErrorString(e));
+  return MM_OK;
+}
+
+mm_status mm_quantize_act_grouped(const void* x_bf16, int64_t ldx, int64_t top_k, const int32_t* perm,
+                                  int64_t perm_stride, const mm_row_groups* groups, const mm_mx_tensor* out,
+                                  void* stream) {
+  g_err[0] = 0;
+  const char* who = "mm_quantize_act_grouped";
+  if (!x_bf16) return fail(MM_ERR_NULL, "%s: input pointer is NULL", who);
+  mm_status st = check_groups(groups, who);
+  if (st != MM_OK) return st;
+  st = check_tensor(out, "out");
+  if (st != MM_OK) return st;
+  st = check_perms(perm, perm_stride, out->K, who);
+  if (st != MM_OK) return st;
+  const mm::GroupLayout gl = mm::group_layout(groups->rows, groups->experts);
+  if (out->rows != gl.capacity)
+    return fail(MM_ERR_SHAPE, "%s: out has %lld rows, the map's capacity is %lld", who, (long long)out->rows,
+                (long long)gl.capacity);
+  if (out->K > kMaxQuantK) return fail(MM_ERR_SHAPE, "%s: K=%lld exceeds %lld", who, (long long)out->K, (long long)kMaxQuantK);
+  if (top_k <= 0 || top_k > mm::kMaxGroupedRows) return fail(MM_ERR_VALUE, "%s: top_k=%lld out of range", who, (long long)top_k);
+  if (ldx < out->K) return fail(MM_ERR_SHAPE, "%s: ld=%lld below K=%lld", who, (long long)ldx, (long long)out->K);
+  if (!aligned16(x_bf16) || ldx % 8 != 0) return fail(MM_ERR_ALIGN, "%s: input must be 16-byte aligned with ld %% 8 == 0", who);
+  const Layout l = layout(out->rows, out->split);
+  mm::QuantGroupedArgs a;
+  a.q = mm::QuantArgs{};
+  a.q.x = static_cast<const uint16_t*>(x_bf16);
+  a.q.ldx = ldx;
+  a.q.perm = perm;
+  a.q.rows = out->rows;
+  a.q.rp = l.rp;
+  a.q.K = (int)out->K;
+  for (int g = 0; g < 3; ++g) {
+    a.q.nb[g] = l.nb[g];
+    a.q.steps[g] = l.steps[g];
+  }
+  a.q.q[0] = out->q4;
+  a.q.q[1] = out->q6;
+  a.q.q[2] = out->q8;
+  a.q.sc = out->sc;
+  a.q.fs = format_set(out);
+  a.perm_stride = perm_stride;
+  a.top_k = (uint32_t)top_k;
+  a.starts = groups->map;
+  a.slots = groups->map + gl.slots;
+  a.owners = groups->map + gl.owners;
+  a.experts = (int)groups->experts;
+  mm::Device dev;
+  hipError_t e = mm::current_device(&dev);
+  if (e == hipSuccess) e = mm::launch_quantize_grouped(a, dev, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return fail(MM_ERR_DEVICE, "%s: launch failed: %s", who, hipGetErrorString(e));
+  return MM_OK;
+}
+
+mm_status mm_gemm_grouped(const mm_mx_tensor* a, const mm_mx_tensor* w, const mm_row_groups* groups, void* y_bf16,
+                          int64_t ldy, void* stream) {
+  g_err[0] = 0;
+  const char* who = "mm_gemm_grouped";
+  mm_status st = check_groups(groups, who);
+  if (st != MM_OK) return st;
+  const mm::GroupLayout gl = mm::group_layout(groups->rows, groups->experts);
+  st = check_product(a, w, y_bf16, ldy, who);
+  if (st != MM_OK) return st;
+  if (a->rows != gl.capacity)
+    return fail(MM_ERR_SHAPE, "%s: a has %lld rows, the map's capacity is %lld", who, (long long)a->rows,
+                (long long)gl.capacity);
+  mm::GemmGroupedArgs g;
+  g.g = gemm_args(a, w, y_bf16, ldy);
+  g.next = expert_stride(w);
+  g.slots = groups->map + gl.slots;
+  for (int k = 0; k < mm::kTileLists; ++k) {
+    g.tiles[k] = tile_list(groups, gl, k);
+    g.ntiles[k] = (int)gl.ntiles[k];
+  }
+  g.rows = groups->rows;
+  g.experts = (int)groups->experts;
+  mm::Device dev;
+  hipError_t e = mm::current_device(&dev);
+  if (e == hipSuccess) e = mm::launch_gemm_grouped(g, dev, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return fail(MM_ERR_DEVICE, "%s: launch failed: %s", who, hipGetErrorString(e));
+  return MM_OK;
+}
+
+mm_status mm_gemv_workspace_size(int64_t rows, int64_t K, mm_split split, int64_t* bytes) {
+  g_err[0] = 0;
+  const char* who = "mm_gemv_workspace_size";
+  if (!bytes) return fail(MM_ERR_NULL, "%s: bytes is NULL", who);
+  mm_status st = check_gemv_rows(rows, who);
+  if (st != MM_OK) return st;
+  st = check_shape(rows, K, split, who);
+  if (st != MM_OK) return st;
+  *bytes = mm::gemv_workspace_bytes(rows, layout(rows, split).steps);
+  return MM_OK;
+}
+
+mm_status mm_gemv(const void* x_bf16, int64_t ldx, int64_t rows, int64_t top_k, const int32_t* perm,
+                  int64_t perm_stride, const mm_mx_tensor* w, int64_t experts, const int32_t* ids, void* workspace,
+                  int64_t workspace_bytes, void* y_bf16, int64_t ldy, void* stream) {
+  g_err[0] = 0;
+  const char* who = "mm_gemv";
+  if (!x_bf16) return fail(MM_ERR_NULL, "%s: input pointer is NULL", who);
+  mm_status st = check_gemv_rows(rows, who);
+  if (st != MM_OK) return st;
+  st = check_group_shape(rows, experts, who);
+  if (st != MM_OK) return st;
+  st = check_tensor(w, "w");
+  if (st != MM_OK) return st;
+  st = check_perms(perm, perm_stride, w->K, who);
+  if (st != MM_OK) return st;
+  if (top_k <= 0 || top_k > mm::kGemvMaxRows) return fail(MM_ERR_VALUE, "%s: top_k=%lld out of range", who, (long long)top_k);
+  if (ldx < w->K) return fail(MM_ERR_SHAPE, "%s: ld=%lld below K=%lld", who, (long long)ldx, (long long)w->K);
+  if ((uintptr_t)x_bf16 & 1u) return fail(MM_ERR_ALIGN, "%s: input must be 2-byte aligned", who);
+  if ((uintptr_t)ids & 3u) return fail(MM_ERR_ALIGN, "%s: ids must be 4-byte aligned", who);
+  st = check_result(w, y_bf16, ldy, who);
+  if (st != MM_OK) return st;
+  const Layout l = layout(w->rows, w->split);
+  const int64_t need = mm::gemv_workspace_bytes(rows, l.steps);
+  if (need > 0 && !workspace) return fail(MM_ERR_NULL, "%s: workspace is NULL", who);
+  if (workspace_bytes < need)
+    return fail(MM_ERR_WORKSPACE, "%s: workspace of %lld bytes, %lld needed", who, (long long)workspace_bytes, (long long)need);
+  if (!aligned16(workspace)) return fail(MM_ERR_ALIGN, "%s: workspace must be 16-byte aligned", who);
+  mm::GemvArgs a;
+  a.x = static_cast<const uint16_t*>(x_bf16);
+  a.ldx = ldx;
+  a.rows = (int)rows;
+  a.top_k = (int)top_k;
+  a.perm = perm;
+  a.perm_stride = perm_stride;
+  a.w = operand(w);
+  a.next = expert_stride(w);
+  a.experts = (int)experts;
+  a.ids = ids;
+  a.K = (int)w->K;
+  for (int g = 0; g < 3; ++g) {
+    a.nb[g] = l.nb[g];
+    a.steps[g] = l.steps[g];
+  }
+  a.y = static_cast<uint16_t*>(y_bf16);
+  a.ldy = ldy;
+  a.fs = format_set(w);
+  a.workspace = workspace;
+  mm::Device dev;
+  hipError_t e = mm::current_device(&dev);
+  if (e == hipSuccess) e = mm::launch_gemv(a, dev, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return fail(MM_ERR_DEVICE, "%s: launch failed: %s", who, hipGetErrorString(e));
+  return MM_OK;
 }
 
 mm_status mm_mx_layout_sizes(int64_t rows, int64_t K, mm_split split, mm_mx_sizes* out) {

@@ -31,8 +31,14 @@
 // Every wavefront works on one group (E2M1, E3M2 or E4M3), the wavefronts
 // shared out by the groups' bytes, so an output's summation order depends on
 // the split and K only, not on the tile shape.
+//
+// The grouped form (mm_gemm_grouped): a tile is a listed run of one expert's packed
+// rows, its weight that expert's; lanes of rows without a slot load the tile's
+// first row again (same cache lines, results never stored), and output rows go
+// where their slots say.
 #include "gemm_common.hpp"
 #include "gemm_route.hpp"
+#include "grouped.hpp"
 
 namespace mm {
 
@@ -106,8 +112,8 @@ __device__ __forceinline__ Desc descs(const Walk& k) {
 // group i of an operand: lane 32 g + r holds row r, as the 32 x 32 x 64 MFMA
 // takes it (E2M1: dwords 0-3 the step's first 64 channels, 4-7 the second).
 template <int G>
-__device__ __forceinline__ v8i load_frag(__amdgpu_buffer_rsrc_t d, int i, int h, int lane) {
-  const int g = lane >> 5, r = lane & 31;
+__device__ __forceinline__ v8i load_frag(__amdgpu_buffer_rsrc_t d, int i, int h, int lane, int r) {
+  const int g = lane >> 5;
   const int off = G == 1 ? g * 768 + r * 24 : g * 512 + r * 16;
   const int at = h * (G == 1 ? 1536 : 2048) + i * (kRowGroup * step_row_bytes(G));
   const u32x4 a = __builtin_amdgcn_raw_buffer_load_b128(d, off, at, 0);
@@ -134,21 +140,35 @@ struct Scales {
   uint32_t w[TN], x[TM];
 };
 
-template <int G, int TN, int TM>
-__device__ __forceinline__ void load_stage(Stage<TN, TM>& b, const Desc& d, int h, int lane) {
+// The activation rows that a tile's loads take: every row of its fragments, or the
+// first n ones (the others take the tile's first row in their place).
+struct AllRows {
+  __device__ __forceinline__ int fragment(int j) const { return j; }
+  __device__ __forceinline__ int row(int, int lane) const { return lane & 31; }
+};
+struct FirstRows {
+  int n;  // at least 1
+  __device__ __forceinline__ int fragment(int j) const { return j == 0 || 32 * j < n ? j : 0; }
+  __device__ __forceinline__ int row(int j, int lane) const { return 32 * j + (lane & 31) < n ? lane & 31 : 0; }
+};
+
+template <int G, int TN, int TM, class Rows>
+__device__ __forceinline__ void load_stage(Stage<TN, TM>& b, const Desc& d, int h, int lane, const Rows& rows) {
 #pragma unroll
-  for (int i = 0; i < TN; ++i) b.w[i] = load_frag<G>(d.w, i, h, lane);
+  for (int i = 0; i < TN; ++i) b.w[i] = load_frag<G>(d.w, i, h, lane, lane & 31);
 #pragma unroll
-  for (int j = 0; j < TM; ++j) b.x[j] = load_frag<G>(d.x, j, h, lane);
+  for (int j = 0; j < TM; ++j) b.x[j] = load_frag<G>(d.x, rows.fragment(j), h, lane, rows.row(j, lane));
 }
 
-template <int TN, int TM>
-__device__ __forceinline__ void load_scales(Scales<TN, TM>& s, const Desc& d, int lane) {
+template <int TN, int TM, class Rows>
+__device__ __forceinline__ void load_scales(Scales<TN, TM>& s, const Desc& d, int lane, const Rows& rows) {
   const int off = (lane & 31) * kStepBlocks;
 #pragma unroll
   for (int i = 0; i < TN; ++i) s.w[i] = __builtin_amdgcn_raw_buffer_load_b32(d.sw, off, i * kRowGroup * kStepBlocks, 0);
 #pragma unroll
-  for (int j = 0; j < TM; ++j) s.x[j] = __builtin_amdgcn_raw_buffer_load_b32(d.sx, off, j * kRowGroup * kStepBlocks, 0);
+  for (int j = 0; j < TM; ++j)
+    s.x[j] = __builtin_amdgcn_raw_buffer_load_b32(d.sx, rows.row(j, lane) * kStepBlocks,
+                                                  rows.fragment(j) * kRowGroup * kStepBlocks, 0);
 }
 
 // Lane 32 g + r feeds the scale of block 2 h + g of its row, h the 64-channel
@@ -184,9 +204,9 @@ __device__ __forceinline__ void mfma_slice(Acc<TN, TM>& acc, const Stage<TN, TM>
 // reloaded as soon as its MFMAs are issued.  The last two are computed
 // without loads behind them (with one step, or an odd number, the last stage
 // is empty: zero codes).
-template <int FS, int TN, int TM>
+template <int FS, int TN, int TM, class Rows>
 __device__ __forceinline__ void run_e2m1(Acc<TN, TM>& acc, const GemmArgs& a, int64_t n0, int64_t m0, int wv, int W,
-                                         int lane) {
+                                         int lane, const Rows& rows) {
   const int n = (a.steps[0] - wv + W - 1) / W;
   if (n <= 0) return;
   Walk k = walk<0>(a, n0, m0, wv, W, n);
@@ -194,8 +214,8 @@ __device__ __forceinline__ void run_e2m1(Acc<TN, TM>& acc, const GemmArgs& a, in
   Scales<TN, TM> s[2];
   auto load = [&](int d) {
     const Desc e = descs(k);
-    load_scales(s[d], e, lane);
-    load_stage<0>(b[d], e, 0, lane);
+    load_scales(s[d], e, lane, rows);
+    load_stage<0>(b[d], e, 0, lane, rows);
     next_step(k);
     __builtin_amdgcn_sched_barrier(0);
   };
@@ -218,19 +238,19 @@ __device__ __forceinline__ void run_e2m1(Acc<TN, TM>& acc, const GemmArgs& a, in
 }
 
 // The same for the E3M2 / E4M3 steps, each two stages (its halves).
-template <int G, int FS, int TN, int TM>
+template <int G, int FS, int TN, int TM, class Rows>
 __device__ __forceinline__ void run_halves(Acc<TN, TM>& acc, const GemmArgs& a, int64_t n0, int64_t m0, int wv, int W,
-                                           int lane) {
+                                           int lane, const Rows& rows) {
   const int n = (a.steps[G] - wv + W - 1) / W;
   if (n <= 0) return;
   Walk k = walk<G>(a, n0, m0, wv, W, n);
   Stage<TN, TM> b0, b1;
   Scales<TN, TM> s;
   Desc e = descs(k);
-  load_scales(s, e, lane);
-  load_stage<G>(b0, e, 0, lane);
+  load_scales(s, e, lane, rows);
+  load_stage<G>(b0, e, 0, lane, rows);
   __builtin_amdgcn_sched_barrier(0);
-  load_stage<G>(b1, e, 1, lane);
+  load_stage<G>(b1, e, 1, lane, rows);
   __builtin_amdgcn_sched_barrier(0);
   for (int i = 1; i < n; ++i) {
     next_step(k);
@@ -239,12 +259,12 @@ __device__ __forceinline__ void run_halves(Acc<TN, TM>& acc, const GemmArgs& a, 
     shift_scales(c, lane);
     mfma_slice<G, FS, 0, 0>(acc, b0, c);
     __builtin_amdgcn_sched_barrier(0);
-    load_scales(s, e, lane);
-    load_stage<G>(b0, e, 0, lane);
+    load_scales(s, e, lane, rows);
+    load_stage<G>(b0, e, 0, lane, rows);
     __builtin_amdgcn_sched_barrier(0);
     mfma_slice<G, FS, 2, 0>(acc, b1, c);
     __builtin_amdgcn_sched_barrier(0);
-    load_stage<G>(b1, e, 1, lane);
+    load_stage<G>(b1, e, 1, lane, rows);
     __builtin_amdgcn_sched_barrier(0);
   }
   shift_scales(s, lane);
@@ -265,30 +285,25 @@ __host__ __device__ constexpr int lds_bytes() {
   return kWaves * TN * reduce_cols<TN, TM>() * 4 * kChunkBytes;
 }
 
-}  // namespace split
+// Where a tile's output rows go: row m to row m of y, rows m_own .. M - 1; or row m
+// to the row that its slot names, the tile's first n rows.
+struct RowsInPlace {
+  int64_t m_own, M;
+  __device__ __forceinline__ int64_t operator()(int64_t m) const { return m < m_own || m >= M ? -1 : m; }
+};
+struct RowsBySlot {
+  const int32_t* slots;
+  int64_t m_own, M;  // M: behind the tile's rows that hold a slot
+  __device__ __forceinline__ int64_t operator()(int64_t m) const { return m >= M ? -1 : slots[m]; }
+};
 
-using namespace split;
-
-template <int TN, int TM, int FS>
-__global__ __launch_bounds__(kThreads) void gemm_split_kernel(GemmArgs a, int tiles_n, int tiles_m, int w0, int w1,
-                                                              int w2) {
-  extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+// One tile: weight rows n0 .. (those from n_own on are its own), activation rows
+// m0 .., wavefronts w0, w1, w2 on the three groups.
+template <int TN, int TM, int FS, class Rows, class Out>
+__device__ __forceinline__ void tile_product(const GemmArgs& a, uint8_t* lds, int64_t n0, int64_t n_own, int64_t m0,
+                                             int w0, int w1, int w2, const Rows& rows, const Out& out) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // workgroup -> tile: consecutive tiles per XCD (workgroups are dealt to the
-  // 8 XCDs round-robin), activation tiles fastest, so the tiles that share a
-  // weight panel run on one XCD
-  const int nt = tiles_n * tiles_m;
-  const int xcd = blockIdx.x & 7, k = blockIdx.x >> 3;
-  const int per_x = nt >> 3, extra = nt & 7;
-  const int id = xcd * per_x + (xcd < extra ? xcd : extra) + k;
-  const int tn = id / tiles_m, tm = id - tn * tiles_m;
-  // the last tile of each direction starts early enough to lie inside the
-  // padded rows; the outputs it shares with the tile before are stored by that one
-  const int64_t n_own = (int64_t)tn * (32 * TN), m_own = (int64_t)tm * (32 * TM);
-  const int64_t n0 = n_own + 32 * TN <= a.w.rp ? n_own : a.w.rp - 32 * TN;
-  const int64_t m0 = m_own + 32 * TM <= a.x.rp ? m_own : a.x.rp - 32 * TM;
-
   Acc<TN, TM> acc;
 #pragma unroll
   for (int i = 0; i < TN; ++i)
@@ -297,9 +312,9 @@ __global__ __launch_bounds__(kThreads) void gemm_split_kernel(GemmArgs a, int ti
 #pragma unroll
       for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
 
-  if (wave < w0) run_e2m1<FS, TN, TM>(acc, a, n0, m0, wave, w0, lane);
-  else if (wave < w0 + w1) run_halves<1, FS, TN, TM>(acc, a, n0, m0, wave - w0, w1, lane);
-  else if (wave < w0 + w1 + w2) run_halves<2, FS, TN, TM>(acc, a, n0, m0, wave - w0 - w1, w2, lane);
+  if (wave < w0) run_e2m1<FS, TN, TM>(acc, a, n0, m0, wave, w0, lane, rows);
+  else if (wave < w0 + w1) run_halves<1, FS, TN, TM>(acc, a, n0, m0, wave - w0, w1, lane, rows);
+  else if (wave < w0 + w1 + w2) run_halves<2, FS, TN, TM>(acc, a, n0, m0, wave - w0 - w1, w2, lane, rows);
 
   // Partial sums through LDS, JC activation fragments at a time.  Wavefront
   // w's words of fragment (i, j): four chunks (registers 4h .. 4h+3), lane
@@ -308,7 +323,7 @@ __global__ __launch_bounds__(kThreads) void gemm_split_kernel(GemmArgs a, int ti
   // stores them as one 16-byte word; consecutive threads take one row's words.
   constexpr int JC = reduce_cols<TN, TM>();
   constexpr int kRowWords = 4 * TN;  // 16-byte output words per row of the tile
-  const int64_t M = a.x.rows, N = a.w.rows;
+  const int64_t N = a.w.rows;
 #pragma unroll
   for (int j0 = 0; j0 < TM; j0 += JC) {
     if (j0) __syncthreads();
@@ -332,7 +347,9 @@ __global__ __launch_bounds__(kThreads) void gemm_split_kernel(GemmArgs a, int ti
       const int row = e / kRowWords, word = e - row * kRowWords;
       const int i = word >> 2, h = word & 3, j = row >> 5, r = row & 31;
       const int64_t m = m0 + 32 * j0 + row, n = n0 + 8 * word;
-      if (j0 + j >= TM || m < m_own || m >= M || n < n_own || n >= N) continue;
+      if (j0 + j >= TM || n < n_own || n >= N) continue;
+      const int64_t to = out(m);
+      if (to < 0) continue;
       v4f lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
@@ -341,7 +358,7 @@ __global__ __launch_bounds__(kThreads) void gemm_split_kernel(GemmArgs a, int ti
         lo = w == 0 ? cl : lo + cl;
         hi = w == 0 ? ch : hi + ch;
       }
-      uint16_t* dst = a.y + m * a.ldy + n;
+      uint16_t* dst = a.y + to * a.ldy + n;
       const u32x4 v = {pack_bf16x2_rne(lo[0], lo[1]), pack_bf16x2_rne(lo[2], lo[3]), pack_bf16x2_rne(hi[0], hi[1]),
                        pack_bf16x2_rne(hi[2], hi[3])};
       if (n + 8 <= N) {
@@ -351,6 +368,54 @@ __global__ __launch_bounds__(kThreads) void gemm_split_kernel(GemmArgs a, int ti
       }
     }
   }
+}
+
+}  // namespace split
+
+using namespace split;
+
+// workgroup -> tile: consecutive tiles per XCD (workgroups are dealt to the
+// 8 XCDs round-robin), activation tiles fastest, so the tiles that share a
+// weight panel run on one XCD
+__device__ __forceinline__ int tile_of(int nt) {
+  const int xcd = blockIdx.x & 7, k = blockIdx.x >> 3;
+  const int per_x = nt >> 3, extra = nt & 7;
+  return xcd * per_x + (xcd < extra ? xcd : extra) + k;
+}
+
+template <int TN, int TM, int FS>
+__global__ __launch_bounds__(kThreads) void gemm_split_kernel(GemmArgs a, int tiles_n, int tiles_m, int w0, int w1,
+                                                              int w2) {
+  extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+  const int id = tile_of(tiles_n * tiles_m);
+  const int tn = id / tiles_m, tm = id - tn * tiles_m;
+  // the last tile of each direction starts early enough to lie inside the
+  // padded rows; the outputs it shares with the tile before are stored by that one
+  const int64_t n_own = (int64_t)tn * (32 * TN), m_own = (int64_t)tm * (32 * TM);
+  const int64_t n0 = n_own + 32 * TN <= a.w.rp ? n_own : a.w.rp - 32 * TN;
+  const int64_t m0 = m_own + 32 * TM <= a.x.rp ? m_own : a.x.rp - 32 * TM;
+  tile_product<TN, TM, FS>(a, lds, n0, n_own, m0, w0, w1, w2, AllRows{}, RowsInPlace{m_own, a.x.rows});
+}
+
+// tiles_m: the length of the tile list, known to the host; how many of its tiles
+// there are only the device knows, the others' workgroups end at once.
+template <int TN, int TM, int FS>
+__global__ __launch_bounds__(kThreads) void gemm_split_grouped_kernel(GemmGroupedArgs a, const RowTile* tiles, int tiles_n,
+                                                                      int tiles_m, int w0, int w1, int w2) {
+  extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+  const int id = tile_of(tiles_n * tiles_m);
+  const int tn = id / tiles_m, tm = id - tn * tiles_m;
+  const RowTile t = tiles[tm];
+  if (t.first < 0) return;  // uniform
+  const int64_t e = t.owner_rows & 0xFFFF;
+  const int n = (int)(t.owner_rows >> 16);
+  GemmArgs g = a.g;
+#pragma unroll
+  for (int k = 0; k < 3; ++k) g.w.q[k] += e * a.next.q[k];
+  g.w.sc += e * a.next.sc;
+  const int64_t n_own = (int64_t)tn * (32 * TN), m0 = (int64_t)t.first * kRowGroup;
+  const int64_t n0 = n_own + 32 * TN <= g.w.rp ? n_own : g.w.rp - 32 * TN;
+  tile_product<TN, TM, FS>(g, lds, n0, n_own, m0, w0, w1, w2, FirstRows{n}, RowsBySlot{a.slots, m0, m0 + n});
 }
 
 template <int TN, int TM, int FS>
@@ -391,6 +456,50 @@ hipError_t launch_gemm_split(const GemmArgs& a, int shape, const Device& dev, hi
     case 2: return launch_shape<2>(a, dev, stream);
     case 3: return launch_shape<3>(a, dev, stream);
     case 4: return launch_shape<4>(a, dev, stream);
+  }
+  return hipErrorInvalidValue;
+}
+
+// ---- the grouped form ----
+
+template <int I, int FS>
+static hipError_t launch_grouped_fs(const GemmGroupedArgs& a, const Device& dev, hipStream_t stream) {
+  constexpr int TN = kSplitShapes[I].tn, TM = kSplitShapes[I].tm;
+  constexpr int kList = TM == 1 ? 0 : (TM == 2 ? 1 : 2);
+  static_assert(TM == 1 << kList, "a listed tile size");
+  constexpr int lds = lds_bytes<TN, TM>();
+  static DeviceOnce once;
+  hipError_t e = allow_lds(once, dev, reinterpret_cast<const void*>(gemm_split_grouped_kernel<TN, TM, FS>), lds);
+  if (e != hipSuccess) return e;
+  const int64_t tn = (a.g.w.rows + 32 * TN - 1) / (32 * TN), tm = a.ntiles[kList];
+  int w[3];
+  share_waves(a.g.steps, kByteCost, kWaves, w);
+  hipLaunchKernelGGL((gemm_split_grouped_kernel<TN, TM, FS>), dim3((unsigned)(tn * tm)), dim3(kThreads), lds, stream, a,
+                     a.tiles[kList], (int)tn, (int)tm, w[0], w[1], w[2]);
+  return hipGetLastError();
+}
+
+template <int I>
+static hipError_t launch_shape_grouped(const GemmGroupedArgs& a, const Device& dev, hipStream_t stream) {
+  switch (a.g.fs) {
+    case 0: return launch_grouped_fs<I, 0>(a, dev, stream);
+    case 1: return launch_grouped_fs<I, 1>(a, dev, stream);
+    case 2: return launch_grouped_fs<I, 2>(a, dev, stream);
+    case 3: return launch_grouped_fs<I, 3>(a, dev, stream);
+  }
+  return hipErrorInvalidValue;
+}
+
+hipError_t launch_gemm_grouped(const GemmGroupedArgs& a, const Device& dev, hipStream_t stream) {
+  return launch_gemm_split_grouped(a, a.g.w.rp < 64 ? 0 : (a.rows / (a.experts < a.rows ? a.experts : a.rows) > 32 ? 4 : 1), dev, stream);
+}
+
+hipError_t launch_gemm_split_grouped(const GemmGroupedArgs& a, int shape, const Device& dev, hipStream_t stream) {
+  switch (shape) {
+    case 0: return launch_shape_grouped<0>(a, dev, stream);
+    case 1: return launch_shape_grouped<1>(a, dev, stream);
+    case 2: return launch_shape_grouped<2>(a, dev, stream);
+    case 4: return launch_shape_grouped<4>(a, dev, stream);
   }
   return hipErrorInvalidValue;
 }

@@ -1,0 +1,128 @@
+// Host-visible argument structs and launchers of the kernels that work on rows
+// ordered by expert, and of the matrix-vector kernel.
+#pragma once
+
+#include "kernels.hpp"
+
+namespace mm {
+
+constexpr int64_t kMaxExperts = 1024;  // a workgroup keeps one count per expert and wavefront in LDS
+constexpr int64_t kMaxGroupedRows = (int64_t)1 << 26;
+
+// One tile of an expert's rows: its first packed row group, and its expert (low
+// 16 bits) with the number of its rows that hold a slot (high 16 bits).  Row
+// group -1: no tile.
+struct RowTile {
+  int32_t first;
+  uint32_t owner_rows;
+};
+
+// Tiles of 1, 2, 4 and 8 row groups (32, 64, 128, 256 rows) are listed.
+constexpr int kTileLists = 4;
+
+// Slots per workgroup of group_rows: sixteen wavefronts of 64 lanes, a few turns each.
+constexpr int64_t kGroupChunk = 4096;
+constexpr int64_t kGroupMaxBlocks = 128;
+
+// The words (int32) of a row-group map (include/micromix.h): starts, slots and
+// owners, then the tile lists and the workgroups' counts.
+struct GroupLayout {
+  int64_t capacity;          // packed rows
+  int64_t slots, owners;     // word offsets
+  int64_t tiles[kTileLists], ntiles[kTileLists];
+  int64_t counts, blocks;    // [blocks, experts], only with more than one workgroup
+  int64_t words;
+};
+
+inline GroupLayout group_layout(int64_t rows, int64_t experts) {
+  auto round4 = [](int64_t v) { return (v + 3) / 4 * 4; };
+  GroupLayout l;
+  const int64_t most = experts < rows ? experts : rows;  // experts that can have rows
+  l.capacity = (rows + (kRowGroup - 1) * most) / kRowGroup * kRowGroup;
+  const int64_t groups = l.capacity / kRowGroup;
+  l.slots = round4(experts + 1);
+  l.owners = l.slots + l.capacity;
+  int64_t at = l.owners + round4(groups);
+  for (int k = 0; k < kTileLists; ++k) {
+    l.tiles[k] = at;
+    // sum over experts of ceil(groups / 2^k): no more than this, and than the groups
+    const int64_t n = (groups >> k) + most;
+    l.ntiles[k] = n < groups ? n : groups;
+    at += round4(2 * l.ntiles[k]);
+  }
+  int64_t b = (rows + kGroupChunk - 1) / kGroupChunk;
+  l.blocks = b > kGroupMaxBlocks ? kGroupMaxBlocks : b;
+  l.counts = at;
+  if (l.blocks > 1) at += round4(l.blocks * experts);
+  l.words = at;
+  return l;
+}
+
+struct GroupArgs {
+  const int32_t* ids;
+  int64_t rows;
+  int experts;
+  int32_t *starts, *slots, *owners, *counts;
+  RowTile* tiles[kTileLists];
+  int ntiles[kTileLists];
+  int groups;   // row groups of the capacity
+  int blocks;   // workgroups
+  int turns;    // ids per lane: a wavefront takes 64 * turns consecutive slots
+};
+hipError_t launch_group_rows(const GroupArgs& a, const Device& dev, hipStream_t stream);
+
+// Quantiser over packed rows: row p takes slot slots[p] (none: nothing is
+// written), that is row slot / top_k of x.
+struct QuantGroupedArgs {
+  QuantArgs q;  // rows = rp = capacity; perm expert 0's
+  int64_t perm_stride;
+  uint32_t top_k;
+  const int32_t *starts, *slots, *owners;
+  int experts;
+};
+hipError_t launch_quantize_grouped(const QuantGroupedArgs& a, const Device& dev, hipStream_t stream);
+
+// Bytes from one expert's weight to the next in each of its buffers.
+struct ExpertStride {
+  int64_t q[3], sc;
+};
+
+struct GemmGroupedArgs {
+  GemmArgs g;  // w: expert 0; x: the packed rows
+  ExpertStride next;
+  const int32_t* slots;
+  const RowTile* tiles[kTileLists];
+  int ntiles[kTileLists];
+  int64_t rows;  // slots
+  int experts;
+};
+hipError_t launch_gemm_grouped(const GemmGroupedArgs& a, const Device& dev, hipStream_t stream);
+hipError_t launch_gemm_split_grouped(const GemmGroupedArgs& a, int shape, const Device& dev, hipStream_t stream);
+
+// At most this many rows in a call of the matrix-vector kernel.
+constexpr int kGemvMaxRows = 16;
+
+struct GemvArgs {
+  const uint16_t* x;
+  int64_t ldx;
+  int rows;
+  int top_k;
+  const int32_t* perm;
+  int64_t perm_stride;
+  Operand w;  // expert 0
+  ExpertStride next;
+  int experts;
+  const int32_t* ids;  // null: every row takes weight 0
+  int K;
+  int nb[3], steps[3];
+  uint16_t* y;
+  int64_t ldy;
+  int fs;
+  void* workspace;  // gemv_workspace_bytes(rows, steps)
+};
+inline int64_t gemv_workspace_bytes(int64_t rows, const int* steps) {
+  return rows * 256 * ((int64_t)steps[0] + steps[1] + steps[2]);
+}
+hipError_t launch_gemv(const GemvArgs& a, const Device& dev, hipStream_t stream);
+
+}  // namespace mm
