@@ -545,13 +545,13 @@ def gemv(x: torch.Tensor, w: MXTensor | MXStack, perm: torch.Tensor, ids: torch.
     stride = _check_perms(perm, experts, K, index)
     need = gemv_workspace_size(rows, K, w.split)
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        workspace = torch.empty(need, dtype=torch.uint8, device=device) if need else None
     elif not workspace.is_contiguous() or workspace.get_device() != index:
         raise ValueError("workspace must be contiguous and on x's device")
     y = _result(y, rows, w.rows, index, device)
     _check(_fast.mm_gemv(x.data_ptr(), x.stride(0), rows, top_k, perm.data_ptr(), stride, w._packed(),
-                         experts, 0 if ids is None else ids.data_ptr(), workspace.data_ptr(), workspace.nbytes,
-                         y.data_ptr(), y.stride(0), _stream_int(stream)))
+                         experts, 0 if ids is None else ids.data_ptr(), 0 if workspace is None else workspace.data_ptr(),
+                         0 if workspace is None else workspace.nbytes, y.data_ptr(), y.stride(0), _stream_int(stream)))
     return y
 
 

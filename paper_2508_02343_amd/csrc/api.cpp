@@ -10,6 +10,7 @@
 #include "../../include/micromix.h"
 #include "gemm_route.hpp"
 #include "grouped.hpp"
+#include "grouped_route.hpp"
 #include "kernels.hpp"
 
 namespace {
@@ -404,6 +405,17 @@ mm::ExpertStride expert_stride(const mm_mx_tensor* w) {
   return mm::ExpertStride{{l.bytes[0], l.bytes[1], l.bytes[2]}, l.bytes[3]};
 }
 
+mm::GemmRoute route_grouped(const mm::GemmGroupedArgs& g, const mm::Device& dev) {
+  mm::GroupedSizes sizes = {g.rows, g.experts, g.g.w.rows, {g.g.steps[0], g.g.steps[1], g.g.steps[2]}, dev.cus, {}};
+  for (int k = 0; k < mm::kTileLists; ++k) sizes.ntiles[k] = g.ntiles[k];
+  return mm::grouped_route(sizes);
+}
+
+hipError_t launch_gemm_grouped(const mm::GemmGroupedArgs& g, const mm::GemmRoute& r, const mm::Device& dev, hipStream_t s) {
+  if (r.kernel == mm::GemmKernel::kSplit) return mm::launch_gemm_split_grouped(g, r.shape, dev, s);
+  return mm::launch_gemm_tiled_grouped(g, r.kernel == mm::GemmKernel::kTiled256, dev, s);
+}
+
 }  // namespace
 
 mm_status mm_group_layout_sizes(int64_t rows, int64_t experts, mm_group_sizes* out) {
@@ -434,6 +446,7 @@ mm_status mm_group_rows(const int32_t* ids, const mm_row_groups* out, void* stre
   a.starts = out->map;
   a.slots = out->map + l.slots;
   a.owners = out->map + l.owners;
+  a.tile_counts = out->map + l.tile_counts;
   a.counts = out->map + l.counts;
   for (int k = 0; k < mm::kTileLists; ++k) {
     a.tiles[k] = tile_list(out, l, k);
@@ -441,7 +454,7 @@ mm_status mm_group_rows(const int32_t* ids, const mm_row_groups* out, void* stre
   }
   a.groups = (int)(l.capacity / mm::kRowGroup);
   a.blocks = (int)l.blocks;
-  a.turns = (int)((out->rows + l.blocks * 1024 - 1) / (l.blocks * 1024));
+  a.turns = (int)((out->rows + l.blocks * mm::kGroupThreads - 1) / (l.blocks * mm::kGroupThreads));
   mm::Device dev;
   hipError_t e = mm::current_device(&dev);
   if (e == hipSuccess) e = mm::launch_group_rows(a, dev, static_cast<hipStream_t>(stream));
@@ -491,7 +504,7 @@ mm_status mm_quantize_act_grouped(const void* x_bf16, int64_t ldx, int64_t top_k
   a.top_k = (uint32_t)top_k;
   a.starts = groups->map;
   a.slots = groups->map + gl.slots;
-  a.owners = groups->map + gl.owners;
+  a.tiles = tile_list(groups, gl, 0);
   a.experts = (int)groups->experts;
   mm::Device dev;
   hipError_t e = mm::current_device(&dev);
@@ -520,11 +533,16 @@ mm_status mm_gemm_grouped(const mm_mx_tensor* a, const mm_mx_tensor* w, const mm
     g.tiles[k] = tile_list(groups, gl, k);
     g.ntiles[k] = (int)gl.ntiles[k];
   }
+  g.counts = groups->map + gl.tile_counts;
   g.rows = groups->rows;
   g.experts = (int)groups->experts;
   mm::Device dev;
   hipError_t e = mm::current_device(&dev);
-  if (e == hipSuccess) e = mm::launch_gemm_grouped(g, dev, static_cast<hipStream_t>(stream));
+  if (e == hipSuccess) {
+    const mm::GemmRoute r = route_grouped(g, dev);
+    if (r.shape < 0) return fail(MM_ERR_SHAPE, "%s: more tiles than a launch takes", who);
+    e = launch_gemm_grouped(g, r, dev, static_cast<hipStream_t>(stream));
+  }
   if (e != hipSuccess) return fail(MM_ERR_DEVICE, "%s: launch failed: %s", who, hipGetErrorString(e));
   return MM_OK;
 }
@@ -537,7 +555,7 @@ mm_status mm_gemv_workspace_size(int64_t rows, int64_t K, mm_split split, int64_
   if (st != MM_OK) return st;
   st = check_shape(rows, K, split, who);
   if (st != MM_OK) return st;
-  *bytes = mm::gemv_workspace_bytes(rows, layout(rows, split).steps);
+  *bytes = mm::gemv_workspace_bytes(rows, K, layout(rows, split).steps);
   return MM_OK;
 }
 
@@ -562,7 +580,7 @@ mm_status mm_gemv(const void* x_bf16, int64_t ldx, int64_t rows, int64_t top_k, 
   st = check_result(w, y_bf16, ldy, who);
   if (st != MM_OK) return st;
   const Layout l = layout(w->rows, w->split);
-  const int64_t need = mm::gemv_workspace_bytes(rows, l.steps);
+  const int64_t need = mm::gemv_workspace_bytes(rows, w->K, l.steps);
   if (need > 0 && !workspace) return fail(MM_ERR_NULL, "%s: workspace is NULL", who);
   if (workspace_bytes < need)
     return fail(MM_ERR_WORKSPACE, "%s: workspace of %lld bytes, %lld needed", who, (long long)workspace_bytes, (long long)need);

@@ -465,7 +465,7 @@ hipError_t launch_gemm_split(const GemmArgs& a, int shape, const Device& dev, hi
 template <int I, int FS>
 static hipError_t launch_grouped_fs(const GemmGroupedArgs& a, const Device& dev, hipStream_t stream) {
   constexpr int TN = kSplitShapes[I].tn, TM = kSplitShapes[I].tm;
-  constexpr int kList = TM == 1 ? 0 : (TM == 2 ? 1 : 2);
+  constexpr int kList = TM == 1 ? 0 : 2;
   static_assert(TM == 1 << kList, "a listed tile size");
   constexpr int lds = lds_bytes<TN, TM>();
   static DeviceOnce once;
@@ -490,15 +490,10 @@ static hipError_t launch_shape_grouped(const GemmGroupedArgs& a, const Device& d
   return hipErrorInvalidValue;
 }
 
-hipError_t launch_gemm_grouped(const GemmGroupedArgs& a, const Device& dev, hipStream_t stream) {
-  return launch_gemm_split_grouped(a, a.g.w.rp < 64 ? 0 : (a.rows / (a.experts < a.rows ? a.experts : a.rows) > 32 ? 4 : 1), dev, stream);
-}
-
 hipError_t launch_gemm_split_grouped(const GemmGroupedArgs& a, int shape, const Device& dev, hipStream_t stream) {
   switch (shape) {
     case 0: return launch_shape_grouped<0>(a, dev, stream);
     case 1: return launch_shape_grouped<1>(a, dev, stream);
-    case 2: return launch_shape_grouped<2>(a, dev, stream);
     case 4: return launch_shape_grouped<4>(a, dev, stream);
   }
   return hipErrorInvalidValue;

@@ -55,7 +55,10 @@
 // codes 507: power is a part of what bounds it).  Without loads and LDS reads,
 // but with the launch, the set-up and the epilogue of every tile: 19.0 (2048 x
 // 4096 x 4096, of which the K loop's MFMAs are 9-10), 430 (8192 x 5120 x 27648).
+#include <type_traits>
+
 #include "gemm_common.hpp"
+#include "grouped.hpp"
 
 namespace mm {
 
@@ -633,9 +636,38 @@ __device__ __forceinline__ void produce(const Ctx<BN, BM>& c) {
 
 using namespace tiled;
 
-template <int BN, int BM, int FS>
-__global__ __launch_bounds__((Tile<BN, BM>::kThreads), 1) void gemm_tiled_kernel(GemmArgs a, int tiles_n, int tiles_m) {
+// What a product's arguments are to a tile: for mm_gemm the operands as they are,
+// activation tiles one after the other; for mm_gemm_grouped one listed run of an
+// expert's packed rows and that expert's weight, output rows where the slots say.
+struct Plain {
+  GemmArgs g;
+  int tiles_n, tiles_m;
+};
+struct Grouped {
+  GemmGroupedArgs g;
+  int tiles_n;
+  const RowTile* tiles;
+  const int32_t* count;  // activation tiles that there are: only the device knows
+};
+
+// Args: Plain or Grouped (the grid covers as many tiles as there may be; the
+// workgroups past those that there are end at once, so that the tiles go evenly to
+// the XCDs).
+template <int BN, int BM, int FS, class Args>
+__global__ __launch_bounds__((Tile<BN, BM>::kThreads), 1) void gemm_tiled_kernel(Args args) {
   using T = Tile<BN, BM>;
+  constexpr bool kGrouped = std::is_same_v<Args, Grouped>;
+  GemmArgs a;
+  const int tiles_n = args.tiles_n;
+  int tiles_m;
+  if constexpr (kGrouped) {
+    tiles_m = *args.count;
+    if ((int)blockIdx.x >= tiles_n * tiles_m) return;  // uniform
+    a = args.g.g;
+  } else {
+    tiles_m = args.tiles_m;
+    a = args.g;
+  }
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
   constexpr int kGroupN = 4;  // weight tiles that share an XCD's L2 at a time
 
@@ -652,7 +684,20 @@ __global__ __launch_bounds__((Tile<BN, BM>::kThreads), 1) void gemm_tiled_kernel
   const int gn = tiles_n - grp * kGroupN < kGroupN ? tiles_n - grp * kGroupN : kGroupN;
   const int tn = grp * kGroupN + within % gn;
   const int tm = within / gn;
-  const int64_t n0 = (int64_t)tn * BN, m0 = (int64_t)tm * BM;
+  const int64_t n0 = (int64_t)tn * BN;
+  int64_t m0 = (int64_t)tm * BM;
+  int64_t x_rows = a.x.rp;  // activation rows that may be read
+  int filled = 0;           // grouped: rows of the tile that hold a slot
+  if constexpr (kGrouped) {
+    const RowTile t = args.tiles[tm];
+    const int64_t e = t.owner_rows & 0xFFFF;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) a.w.q[k] += e * args.g.next.q[k];
+    a.w.sc += e * args.g.next.sc;
+    m0 = (int64_t)t.first * kRowGroup;
+    filled = (int)(t.owner_rows >> 16);
+    x_rows = m0 + (filled + kRowGroup - 1) / kRowGroup * kRowGroup;
+  }
 
   Ctx<BN, BM> c;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // uniform: keeps DMA setup scalar
@@ -669,17 +714,17 @@ __global__ __launch_bounds__((Tile<BN, BM>::kThreads), 1) void gemm_tiled_kernel
 
   DmaConst& k = c.k;
   k.wave = w4;
-  auto codes = [&](DmaCodes& d, const Operand& o, int64_t r0) {  // r0: the tile's first row (below its padded rows - 31)
+  auto codes = [&](DmaCodes& d, const Operand& o, int64_t r0, int64_t rp) {  // r0: the tile's first row (below rp - 31)
     d.code0 = o.q[0] + r0 * step_row_bytes(0);
     d.code1 = o.q[1] + r0 * step_row_bytes(1);
     d.code2 = o.q[2] + r0 * step_row_bytes(2);
     d.rstride0 = o.rp * step_row_bytes(0);
     d.rstride1 = o.rp * step_row_bytes(1);
     d.rstride2 = o.rp * step_row_bytes(2);
-    d.last = (int)(o.rp / kRowGroup - r0 / kRowGroup - 1);
+    d.last = (int)(rp / kRowGroup - r0 / kRowGroup - 1);
   };
-  codes(k.w, a.w, n0);
-  codes(k.x, a.x, m0);
+  codes(k.w, a.w, n0, a.w.rp);
+  codes(k.x, a.x, m0, x_rows);
   k.w.lds = k.w.lds6 = 0;
   k.x.lds = BN / kRowGroup * 2048;
   k.x.lds6 = BN / kRowGroup * 1536;
@@ -690,7 +735,8 @@ __global__ __launch_bounds__((Tile<BN, BM>::kThreads), 1) void gemm_tiled_kernel
   // 4 rows per lane; rows past the padded rows re-read the last 4
   const int per = (op ? BM : BN) / 2;
   int64_t row = half * per + c.lane * 4;  // row within the tile
-  row = r0 + row + 4 <= o.rp ? row : o.rp - 4 - r0;
+  const int64_t o_rows = kGrouped && op ? x_rows : o.rp;
+  row = r0 + row + 4 <= o_rows ? row : o_rows - 4 - r0;
   k.soff = (uint32_t)row * kStepBlocks;
   k.sdst = (uint32_t)(T::kScaleOff + (op ? BN * kStepBlocks : 0) + half * per * kStepBlocks);
   k.smask = per / 4 >= 64 ? ~0ull : ((1ull << (per / 4)) - 1);
@@ -754,8 +800,11 @@ __global__ __launch_bounds__((Tile<BN, BM>::kThreads), 1) void gemm_tiled_kernel
   const int64_t M = a.x.rows, N = a.w.rows;
   for (int ch = threadIdx.x; ch < BM * kChunks; ch += T::kThreads) {
     const int rr = ch / kChunks, col = (ch - rr * kChunks) * 8;
-    const int64_t m = m0 + rr, n = n0 + col;
-    if (m >= M || n >= N) continue;
+    int64_t m = m0 + rr;
+    const int64_t n = n0 + col;
+    if (kGrouped ? rr >= filled : m >= M) continue;
+    if (n >= N) continue;
+    if constexpr (kGrouped) m = args.g.slots[m];
     const u32x4 v = lds_read<u32x4>(c.lds0 + rr * kRowStride + col * 2);
     uint16_t* dst = a.y + m * a.ldy + n;
     if (n + 8 <= N) {
@@ -771,31 +820,48 @@ __global__ __launch_bounds__((Tile<BN, BM>::kThreads), 1) void gemm_tiled_kernel
   }
 }
 
-template <int BN, int BM, int FS>
-static hipError_t launch_tile_fs(const GemmArgs& a, const Device& dev, hipStream_t stream) {
+template <int BN, int BM, int FS, class Args>
+static hipError_t launch_tile_fs(const Args& a, int64_t tiles, const Device& dev, hipStream_t stream) {
   static DeviceOnce once;
-  hipError_t e = allow_lds(once, dev, reinterpret_cast<const void*>(gemm_tiled_kernel<BN, BM, FS>), kLdsBytes);
+  hipError_t e = allow_lds(once, dev, reinterpret_cast<const void*>(gemm_tiled_kernel<BN, BM, FS, Args>), kLdsBytes);
   if (e != hipSuccess) return e;
-  const int tn = (int)((a.w.rows + BN - 1) / BN), tm = (int)((a.x.rows + BM - 1) / BM);
-  hipLaunchKernelGGL((gemm_tiled_kernel<BN, BM, FS>), dim3((unsigned)(tn * tm)), dim3(Tile<BN, BM>::kThreads), kLdsBytes, stream, a,
-                     tn, tm);
+  hipLaunchKernelGGL((gemm_tiled_kernel<BN, BM, FS, Args>), dim3((unsigned)tiles), dim3(Tile<BN, BM>::kThreads), kLdsBytes,
+                     stream, a);
   return hipGetLastError();
 }
 
 // The format set is an instruction immediate: one kernel per set.
-template <int BN, int BM>
-static hipError_t launch_tile(const GemmArgs& a, const Device& dev, hipStream_t stream) {
-  switch (a.fs) {
-    case 0: return launch_tile_fs<BN, BM, 0>(a, dev, stream);
-    case 1: return launch_tile_fs<BN, BM, 1>(a, dev, stream);
-    case 2: return launch_tile_fs<BN, BM, 2>(a, dev, stream);
-    case 3: return launch_tile_fs<BN, BM, 3>(a, dev, stream);
+template <int BN, int BM, class Args>
+static hipError_t launch_tile(const Args& a, int fs, int64_t tiles, const Device& dev, hipStream_t stream) {
+  switch (fs) {
+    case 0: return launch_tile_fs<BN, BM, 0>(a, tiles, dev, stream);
+    case 1: return launch_tile_fs<BN, BM, 1>(a, tiles, dev, stream);
+    case 2: return launch_tile_fs<BN, BM, 2>(a, tiles, dev, stream);
+    case 3: return launch_tile_fs<BN, BM, 3>(a, tiles, dev, stream);
   }
   return hipErrorInvalidValue;
 }
 
+template <int BN, int BM>
+static hipError_t launch_plain(const GemmArgs& g, const Device& dev, hipStream_t stream) {
+  const Plain a = {g, (int)((g.w.rows + BN - 1) / BN), (int)((g.x.rows + BM - 1) / BM)};
+  return launch_tile<BN, BM>(a, g.fs, (int64_t)a.tiles_n * a.tiles_m, dev, stream);
+}
+
+template <int BN, int BM>
+static hipError_t launch_grouped(const GemmGroupedArgs& g, const Device& dev, hipStream_t stream) {
+  constexpr int kList = BM == 128 ? 2 : 3;
+  static_assert(BM == kRowGroup << kList, "a listed tile size");
+  const Grouped a = {g, (int)((g.g.w.rows + BN - 1) / BN), g.tiles[kList], g.counts + kList};
+  return launch_tile<BN, BM>(a, g.g.fs, (int64_t)a.tiles_n * g.ntiles[kList], dev, stream);
+}
+
 hipError_t launch_gemm_tiled(const GemmArgs& a, bool square, const Device& dev, hipStream_t stream) {
-  return square ? launch_tile<256, 256>(a, dev, stream) : launch_tile<256, 128>(a, dev, stream);
+  return square ? launch_plain<256, 256>(a, dev, stream) : launch_plain<256, 128>(a, dev, stream);
+}
+
+hipError_t launch_gemm_tiled_grouped(const GemmGroupedArgs& a, bool square, const Device& dev, hipStream_t stream) {
+  return square ? launch_grouped<256, 256>(a, dev, stream) : launch_grouped<256, 128>(a, dev, stream);
 }
 
 }  // namespace mm

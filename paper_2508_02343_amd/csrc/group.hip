@@ -6,17 +6,17 @@
 // 4 out per slot.  Every wavefront takes a run of consecutive slots, 64 at a
 // time.  A lane's rank among the 64 is the number of lower lanes with its expert:
 // one ballot per bit of the expert number gives every lane the mask of its equals,
-// so there are no atomics and the order never depends on timing.  The counts
-// per wavefront and expert sit in LDS; their sums over the wavefronts in front
-// and the padded starts make them the next free row of that wavefront and
-// expert.  More than kGroupChunk slots: a first launch leaves each workgroup's
-// counts, the second places.
+// so the order never depends on timing (atomics only add up counts).  The
+// counts per wavefront and expert sit in LDS; their sums over the wavefronts in
+// front and the padded starts give every wavefront its first row of each expert.
+// More than kGroupChunk slots: a first launch leaves each workgroup's counts, the
+// second places.
 #include "grouped.hpp"
 
 namespace mm {
 namespace {
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64;
+constexpr int kThreads = kGroupThreads, kWaves = kThreads / 64;
 
 // Lanes whose key (below 2^bits) equals this lane's.
 __device__ __forceinline__ uint64_t equals(int key, int bits) {
@@ -35,17 +35,8 @@ __device__ __forceinline__ int key_of(const GroupArgs& a, int64_t slot) {
   return (unsigned)id < (unsigned)a.experts ? id : a.experts;
 }
 
-// Adds the slots of each expert in this wavefront's run to n[expert].
-__device__ __forceinline__ void count_run(const GroupArgs& a, int64_t first, int bits, uint32_t* n, int lane) {
-  for (int t = 0; t < a.turns; ++t) {
-    const int64_t s0 = first + 64 * (int64_t)t;
-    if (s0 >= a.rows) break;
-    const int key = key_of(a, s0 + lane);
-    const uint64_t m = equals(key, bits);
-    if (key < a.experts && (m & ((1ull << lane) - 1)) == 0) n[key] += (uint32_t)__popcll(m);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  }
-}
+// Turns of a wavefront that fit in registers.
+constexpr int kTurns = (int)(kGroupChunk / kThreads);
 
 // Inclusive sum over the workgroup's threads of each of N values.
 template <int N>
@@ -68,21 +59,18 @@ __device__ __forceinline__ void scan(int (&v)[N], int (*part)[N], int lane, int 
 }  // namespace
 
 // Each workgroup's slots per expert.
-__global__ __launch_bounds__(kThreads) void group_count_kernel(GroupArgs a, int bits) {
-  extern __shared__ uint32_t lds[];  // [kWaves][experts]
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+__global__ __launch_bounds__(kThreads) void group_count_kernel(GroupArgs a) {
+  extern __shared__ uint32_t lds[];  // [experts]
   const int E = a.experts;
-  for (int i = threadIdx.x; i < kWaves * E; i += kThreads) lds[i] = 0;
+  if ((int)threadIdx.x < E) lds[threadIdx.x] = 0;
   __syncthreads();
-  const int64_t run = ((int64_t)blockIdx.x * kWaves + wave) * 64 * a.turns;
-  count_run(a, run, bits, lds + wave * E, lane);
-  __syncthreads();
-  const int e = threadIdx.x;
-  if (e < E) {
-    uint32_t n = 0;
-    for (int w = 0; w < kWaves; ++w) n += lds[w * E + e];
-    a.counts[(int64_t)blockIdx.x * E + e] = (int32_t)n;
+  const int64_t s0 = (int64_t)blockIdx.x * kThreads * a.turns + threadIdx.x;
+  for (int t = 0; t < a.turns; ++t) {
+    const int key = key_of(a, s0 + (int64_t)t * kThreads);
+    if (key < E) atomicAdd(&lds[key], 1u);  // (a count: the order does not matter)
   }
+  __syncthreads();
+  if ((int)threadIdx.x < E) a.counts[(int64_t)blockIdx.x * E + threadIdx.x] = (int32_t)lds[threadIdx.x];
 }
 
 // Places the slots; the rows, owners and tiles that no slot fills are shared out
@@ -92,14 +80,53 @@ __global__ __launch_bounds__(kThreads) void group_place_kernel(GroupArgs a, int 
   const int E = a.experts;
   uint32_t* const next = lds;                            // [kWaves][E]
   int* const total = (int*)(lds + kWaves * E);           // [E] slots of each expert
-  int* const start = total + E;                          // [E + 1] first row group
+  int* const front = total + E;                          // [E] those of the workgroups in front
+  int* const start = front + E;                          // [E + 1] first row group
   int* const tile0 = start + E + 1;                      // [3][E] first tile of 2, 4, 8 row groups
   int (*const part)[kTileLists] = (int (*)[kTileLists])(tile0 + 3 * E);  // [kWaves]
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int i = threadIdx.x; i < kWaves * E; i += kThreads) next[i] = 0;
-  __syncthreads();
   const int64_t run = ((int64_t)blockIdx.x * kWaves + wave) * 64 * a.turns;
-  count_run(a, run, bits, next + wave * E, lane);
+  int key[kTurns], rank[kTurns];
+  const bool kept = a.turns <= kTurns;
+  if (kept)
+#pragma unroll
+    for (int t = 0; t < kTurns; ++t) key[t] = t < a.turns ? key_of(a, run + 64 * t + lane) : E;
+  for (int i = threadIdx.x; i < (kWaves + 2) * E; i += kThreads) next[i] = 0;  // (total and front with them)
+  __syncthreads();
+  uint32_t* const mine = next + wave * E;
+  if (a.blocks > 1) {
+    // every workgroup's counts, in slices of workgroups, several threads to an expert
+    const int slices = kThreads / E, e = threadIdx.x % E, j = threadIdx.x / E;
+    if (j < slices) {
+      int before = 0, all = 0;
+#pragma unroll 8
+      for (int b = j; b < a.blocks; b += slices) {
+        const int n = a.counts[(int64_t)b * E + e];
+        before += b < (int)blockIdx.x ? n : 0;
+        all += n;
+      }
+      atomicAdd(&total[e], all);
+      atomicAdd(&front[e], before);
+    }
+  }
+  // this wavefront's slots of each expert, and a slot's rank among them
+  if (kept) {
+#pragma unroll
+    for (int t = 0; t < kTurns; ++t)
+      if (t < a.turns) {  // uniform
+        const uint64_t m = equals(key[t], bits);
+        const int lower = __popcll(m & ((1ull << lane) - 1));
+        rank[t] = key[t] < E ? (int)mine[key[t]] + lower : 0;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (key[t] < E && lower == 0) mine[key[t]] += (uint32_t)__popcll(m);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      }
+  } else {
+    for (int t = 0; t < a.turns; ++t) {
+      const int k = key_of(a, run + 64 * (int64_t)t + lane);
+      if (k < E) atomicAdd(&mine[k], 1u);
+    }
+  }
   __syncthreads();
   const int e = threadIdx.x;  // kThreads >= kMaxExperts
   int here = 0, before = 0, all = 0;
@@ -109,15 +136,8 @@ __global__ __launch_bounds__(kThreads) void group_place_kernel(GroupArgs a, int 
       next[w * E + e] = (uint32_t)here;
       here += n;
     }
-    all = here;
-    if (a.blocks > 1) {
-      all = 0;
-      for (int b = 0; b < a.blocks; ++b) {
-        const int n = a.counts[(int64_t)b * E + e];
-        before += b < (int)blockIdx.x ? n : 0;
-        all += n;
-      }
-    }
+    before = front[e];
+    all = a.blocks > 1 ? total[e] : here;
   }
   const int g = (all + kRowGroup - 1) / kRowGroup;
   int v[kTileLists] = {g, (g + 1) / 2, (g + 3) / 4, (g + 7) / 8};
@@ -131,23 +151,32 @@ __global__ __launch_bounds__(kThreads) void group_place_kernel(GroupArgs a, int 
     for (int k = 1; k < kTileLists; ++k) tile0[(k - 1) * E + e] = v[k] - own[k];
     if (e == E - 1) {
       start[E] = v[0];
-      if (blockIdx.x == 0) a.starts[E] = v[0] * kRowGroup;
+      if (blockIdx.x == 0) {
+        a.starts[E] = v[0] * kRowGroup;
+#pragma unroll
+        for (int k = 0; k < kTileLists; ++k) a.tile_counts[k] = v[k];
+      }
     }
     if (blockIdx.x == 0) a.starts[e] = s * kRowGroup;
     for (int w = 0; w < kWaves; ++w) next[w * E + e] += (uint32_t)(s * kRowGroup + before);
   }
   __syncthreads();
   // the slots, in their order
-  for (int t = 0; t < a.turns; ++t) {
-    const int64_t s0 = run + 64 * (int64_t)t;
-    if (s0 >= a.rows) break;
-    const int key = key_of(a, s0 + lane);
-    const uint64_t m = equals(key, bits);
-    const int rank = __popcll(m & ((1ull << lane) - 1));
-    if (key < E) a.slots[next[wave * E + key] + rank] = (int32_t)(s0 + lane);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (key < E && rank == 0) next[wave * E + key] += (uint32_t)__popcll(m);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  if (kept) {
+#pragma unroll
+    for (int t = 0; t < kTurns; ++t)
+      if (key[t] < E) a.slots[mine[key[t]] + rank[t]] = (int32_t)(run + 64 * t + lane);
+  } else {
+    for (int t = 0; t < a.turns; ++t) {
+      const int64_t slot = run + 64 * (int64_t)t + lane;
+      const int k = key_of(a, slot);
+      const uint64_t m = equals(k, bits);
+      const int lower = __popcll(m & ((1ull << lane) - 1));
+      if (k < E) a.slots[mine[k] + lower] = (int32_t)slot;
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      if (k < E && lower == 0) mine[k] += (uint32_t)__popcll(m);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
   }
   // the row groups: owner, rows without a slot, tiles
   const int used = start[E];
@@ -181,7 +210,7 @@ __global__ __launch_bounds__(kThreads) void group_place_kernel(GroupArgs a, int 
   // tiles behind the last
 #pragma unroll
   for (int k = 1; k < kTileLists; ++k) {
-    int n = E > 0 ? tile0[(k - 1) * E + E - 1] + ((start[E] - start[E - 1] + (1 << k) - 1) >> k) : 0;
+      const int n = tile0[(k - 1) * E + E - 1] + ((start[E] - start[E - 1] + (1 << k) - 1) >> k);
     for (int i = n + at; i < a.ntiles[k]; i += stride) a.tiles[k][i] = RowTile{-1, 0};
   }
 }
@@ -190,20 +219,16 @@ hipError_t launch_group_rows(const GroupArgs& a, const Device& dev, hipStream_t 
   int bits = 1;
   while ((1 << bits) <= a.experts) ++bits;  // keys 0 .. experts
   const int E = a.experts;
-  const int count_lds = kWaves * E * 4;
-  const int place_lds = (kWaves * E + 5 * E + 1) * 4 + kWaves * kTileLists * 4;
-  constexpr int kMost = (int)((kWaves + 5) * kMaxExperts + 1 + kWaves * kTileLists) * 4;
-  static DeviceOnce once_count, once_place;
-  hipError_t e = allow_lds(once_place, dev, reinterpret_cast<const void*>(group_place_kernel), kMost);
+  auto place_lds = [](int n) { return ((kWaves + 6) * n + 1 + kWaves * kTileLists) * 4; };
+  static DeviceOnce once;
+  hipError_t e = allow_lds(once, dev, reinterpret_cast<const void*>(group_place_kernel), place_lds(kMaxExperts));
   if (e != hipSuccess) return e;
   if (a.blocks > 1) {
-    e = allow_lds(once_count, dev, reinterpret_cast<const void*>(group_count_kernel), kMost);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(group_count_kernel, dim3(a.blocks), dim3(kThreads), count_lds, stream, a, bits);
+    hipLaunchKernelGGL(group_count_kernel, dim3(a.blocks), dim3(kThreads), E * 4, stream, a);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(group_place_kernel, dim3(a.blocks), dim3(kThreads), place_lds, stream, a, bits);
+  hipLaunchKernelGGL(group_place_kernel, dim3(a.blocks), dim3(kThreads), place_lds(E), stream, a, bits);
   return hipGetLastError();
 }
 

@@ -20,7 +20,9 @@ struct RowTile {
 // Tiles of 1, 2, 4 and 8 row groups (32, 64, 128, 256 rows) are listed.
 constexpr int kTileLists = 4;
 
-// Slots per workgroup of group_rows: sixteen wavefronts of 64 lanes, a few turns each.
+// group_rows: one workgroup of 1024 threads up to kGroupChunk slots, above one for
+// every 1024 slots, at most kGroupMaxBlocks.
+constexpr int64_t kGroupThreads = 1024;
 constexpr int64_t kGroupChunk = 4096;
 constexpr int64_t kGroupMaxBlocks = 128;
 
@@ -30,6 +32,7 @@ struct GroupLayout {
   int64_t capacity;          // packed rows
   int64_t slots, owners;     // word offsets
   int64_t tiles[kTileLists], ntiles[kTileLists];
+  int64_t tile_counts;       // [kTileLists]: tiles in each list
   int64_t counts, blocks;    // [blocks, experts], only with more than one workgroup
   int64_t words;
 };
@@ -50,8 +53,10 @@ inline GroupLayout group_layout(int64_t rows, int64_t experts) {
     l.ntiles[k] = n < groups ? n : groups;
     at += round4(2 * l.ntiles[k]);
   }
-  int64_t b = (rows + kGroupChunk - 1) / kGroupChunk;
+  const int64_t b = rows <= kGroupChunk ? 1 : (rows + kGroupThreads - 1) / kGroupThreads;
   l.blocks = b > kGroupMaxBlocks ? kGroupMaxBlocks : b;
+  l.tile_counts = at;
+  at += kTileLists;
   l.counts = at;
   if (l.blocks > 1) at += round4(l.blocks * experts);
   l.words = at;
@@ -62,12 +67,12 @@ struct GroupArgs {
   const int32_t* ids;
   int64_t rows;
   int experts;
-  int32_t *starts, *slots, *owners, *counts;
+  int32_t *starts, *slots, *owners, *tile_counts, *counts;
   RowTile* tiles[kTileLists];
   int ntiles[kTileLists];
   int groups;   // row groups of the capacity
   int blocks;   // workgroups
-  int turns;    // ids per lane: a wavefront takes 64 * turns consecutive slots
+  int turns;    // ids per thread: a wavefront takes 64 * turns consecutive slots
 };
 hipError_t launch_group_rows(const GroupArgs& a, const Device& dev, hipStream_t stream);
 
@@ -77,7 +82,8 @@ struct QuantGroupedArgs {
   QuantArgs q;  // rows = rp = capacity; perm expert 0's
   int64_t perm_stride;
   uint32_t top_k;
-  const int32_t *starts, *slots, *owners;
+  const int32_t *starts, *slots;
+  const RowTile* tiles;  // of one row group
   int experts;
 };
 hipError_t launch_quantize_grouped(const QuantGroupedArgs& a, const Device& dev, hipStream_t stream);
@@ -92,11 +98,13 @@ struct GemmGroupedArgs {
   ExpertStride next;
   const int32_t* slots;
   const RowTile* tiles[kTileLists];
-  int ntiles[kTileLists];
+  int ntiles[kTileLists];  // bounds that the host knows
+  const int32_t* counts;   // [kTileLists] tiles that there are
   int64_t rows;  // slots
   int experts;
 };
-hipError_t launch_gemm_grouped(const GemmGroupedArgs& a, const Device& dev, hipStream_t stream);
+hipError_t launch_gemm_tiled_grouped(const GemmGroupedArgs& a, bool square, const Device& dev, hipStream_t stream);
+// shape: 0, 1 or 4 of kSplitShapes
 hipError_t launch_gemm_split_grouped(const GemmGroupedArgs& a, int shape, const Device& dev, hipStream_t stream);
 
 // At most this many rows in a call of the matrix-vector kernel.
@@ -118,10 +126,17 @@ struct GemvArgs {
   uint16_t* y;
   int64_t ldy;
   int fs;
-  void* workspace;  // gemv_workspace_bytes(rows, steps)
+  void* workspace;  // gemv_workspace_bytes(rows, K, steps)
 };
-inline int64_t gemv_workspace_bytes(int64_t rows, const int* steps) {
-  return rows * 256 * ((int64_t)steps[0] + steps[1] + steps[2]);
+// LDS of a workgroup of `waves` wavefronts that holds `rows` rows of x: the rows, and
+// 64 words of each per wavefront.  Up to kGemvMaxLds with the most wavefronts, x goes
+// that way; beside it the workgroup has 32 KB of sums.
+constexpr int kGemvMaxWaves = 16;
+constexpr int64_t kGemvMaxLds = 110 * 1024;
+inline int64_t gemv_lds_bytes(int64_t rows, int64_t K, int waves) { return rows * (2 * K + 1024 * (int64_t)waves); }
+inline bool gemv_in_lds(int64_t rows, int64_t K) { return gemv_lds_bytes(rows, K, kGemvMaxWaves) <= kGemvMaxLds; }
+inline int64_t gemv_workspace_bytes(int64_t rows, int64_t K, const int* steps) {
+  return gemv_in_lds(rows, K) ? 0 : rows * 256 * ((int64_t)steps[0] + steps[1] + steps[2]);
 }
 hipError_t launch_gemv(const GemvArgs& a, const Device& dev, hipStream_t stream);
 

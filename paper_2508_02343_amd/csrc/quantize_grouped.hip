@@ -5,12 +5,17 @@
 // slot are read and written.
 //
 // HBM-bound: 2 bytes per element in (a token's row is read once per expert that
-// takes it, after the first time from the caches), bits / 8 + 1 / 32 out.  A
-// workgroup takes a run of consecutive passes of RH packed rows, one thread per
-// (row, 32-channel block): the rows go to LDS with 16-byte loads, each thread
-// gathers its block by sigma and writes its codes.  sigma stays in registers
-// until the expert changes, and a run of passes keeps the rows of a 32-row group,
-// which share cache lines in the packed layout, in one L2.
+// takes it, after the first time from the caches), bits / 8 + 1 / 32 out.  As in
+// quantize.hip a workgroup stages a pass of RH packed rows in LDS, one thread per (row,
+// 32-channel block), the next pass's rows in flight while it quantises this one, and
+// the passes that run together on an XCD are neighbours, so that the rows of a 32-row
+// group, which share cache lines in the packed layout, meet in one L2.  sigma stays
+// in registers until the expert changes.
+//
+// Measured (us): 16 rows of K 4096 4.5; 4096 slots x 4096, two per token, 14.9 (2.9
+// TB/s of rows and codes); 8192 slots x 14336, a sigma per expert, 79 (3.9 TB/s).  A run
+// of consecutive passes to each workgroup took 109 on the last (the lines of half-filled
+// row groups do not last in the L2), without the next pass's loads in flight 111.
 #include "grouped.hpp"
 #include "quantize_common.hpp"
 
@@ -33,8 +38,48 @@ __global__ __launch_bounds__(kMaxQuantThreads) void quantize_grouped_kernel(Quan
   const int blk = t / RH, prow = t - blk * RH;
   const uint32_t row_stride = (uint32_t)(2 * K + 16);
 
+  // this workgroup's passes: those of quantize.hip (each XCD a contiguous range, its
+  // workgroups in turn), as far as they have rows
+  constexpr int kPasses = kRowGroup / RH;  // per row group
   const int64_t passes = ga.starts[ga.experts] / RH;  // (a multiple of 32 rows)
-  const int64_t q_end = passes * (blockIdx.x + 1) / gridDim.x;
+  int64_t q, q_end, stride;
+  if (gridDim.x % 8 == 0) {
+    const int x = blockIdx.x & 7;
+    q = passes * x / 8 + (blockIdx.x >> 3);
+    q_end = passes * (x + 1) / 8;
+    stride = gridDim.x / 8;
+  } else {
+    q = blockIdx.x;
+    q_end = passes;
+    stride = gridDim.x;
+  }
+  // Moves q on to a pass with rows, and its row group's tile; an expert's rows come
+  // first in its row groups.
+  RowTile tile = {};
+  auto seek = [&] {  // uniform over the workgroup
+    for (; q < q_end; q += stride) {
+      tile = ga.tiles[q / kPasses];
+      if ((int)(q % kPasses) * RH < (int)(tile.owner_rows >> 16)) return;
+    }
+  };
+  constexpr int kParts = 4 / RH;  // a row's 16-byte chunks over the threads: kParts each
+  u32x4 buf[4];
+  auto load = [&] {
+#pragma unroll
+    for (int j = 0; j < RH; ++j) {
+      int32_t s = ga.slots[q * RH + j];
+      s = s < 0 ? ga.slots[q * RH] : s;  // (rows without a slot: the pass's first again)
+      const int64_t row = (uint32_t)s / ga.top_k;
+#pragma unroll
+      for (int k = 0; k < kParts; ++k) {
+        const uint8_t* src = reinterpret_cast<const uint8_t*>(a.x + row * a.ldx + k * n_act * 8);
+        buf[j * kParts + k] = *reinterpret_cast<const u32x4*>(src + (uint32_t)t * 16u);
+      }
+    }
+  };
+  seek();
+  if (q >= q_end) return;
+  load();
 
   const int group = blk < a.nb[0] ? 0 : (blk < a.nb[0] + a.nb[1] ? 1 : 2);
   const int b = blk - (group >= 1 ? a.nb[0] : 0) - (group >= 2 ? a.nb[1] : 0);
@@ -45,24 +90,16 @@ __global__ __launch_bounds__(kMaxQuantThreads) void quantize_grouped_kernel(Quan
                                                  : a.q[2] + code_offset<2>(b >> 2, a.rp, prow, b & 3)));
   uint8_t* const sdst = a.sc + ((gstep0 + (b >> 2)) * a.rp + prow) * kStepBlocks + (b & 3);
 
-  constexpr int kParts = 4 / RH;  // a row's 16-byte chunks over the threads: kParts each
   uint32_t sig[16] = {};
   int owner = -1;
-  for (int64_t q = passes * blockIdx.x / gridDim.x; q < q_end; ++q) {
+  while (q < q_end) {
     const int64_t row0 = q * RH;
-    int32_t slot[RH];
+    const int e = (int)(tile.owner_rows & 0xFFFF);
+    const bool filled = (int)(q % kPasses) * RH + prow < (int)(tile.owner_rows >> 16);
+    if (active)
 #pragma unroll
-    for (int j = 0; j < RH; ++j) slot[j] = ga.slots[row0 + j];
-    if (slot[0] < 0) continue;  // uniform: an expert's rows come first in its row groups
-    u32x4 buf[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int32_t s = slot[j / kParts] < 0 ? slot[0] : slot[j / kParts];
-      const int64_t row = (uint32_t)s / ga.top_k;
-      const uint8_t* src = reinterpret_cast<const uint8_t*>(a.x + row * a.ldx + j % kParts * n_act * 8);
-      buf[j] = *reinterpret_cast<const u32x4*>(src + (uint32_t)t * 16u);
-    }
-    const int e = ga.owners[row0 / kRowGroup];
+      for (int j = 0; j < 4; ++j)
+        lds_store<u32x4>(lds0 + (uint32_t)(j / kParts) * row_stride + (uint32_t)(j % kParts * n_act + t) * 16u, buf[j]);
     if (e != owner) {
       owner = e;
       const int32_t* perm = a.perm + e * ga.perm_stride;
@@ -77,11 +114,10 @@ __global__ __launch_bounds__(kMaxQuantThreads) void quantize_grouped_kernel(Quan
         sig[2 * k + 1] = o[2] | (o[3] << 16);
       }
     }
-    if (active)
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        lds_store<u32x4>(lds0 + (uint32_t)(j / kParts) * row_stride + (uint32_t)(j % kParts * n_act + t) * 16u, buf[j]);
     __syncthreads();
+    q += stride;
+    seek();
+    if (q < q_end) load();  // in flight while this pass is quantised
     uint32_t base = lds0 + (uint32_t)prow * row_stride;
     asm volatile("" : "+v"(base));  // (see add_word)
     uint32_t d[16];
@@ -102,9 +138,6 @@ __global__ __launch_bounds__(kMaxQuantThreads) void quantize_grouped_kernel(Quan
         d[8 * h + i] = __builtin_bit_cast(uint32_t, w);
       }
     }
-    bool filled = false;
-#pragma unroll
-    for (int j = 0; j < RH; ++j) filled |= prow == j && slot[j] >= 0;
     if (active && filled) encode_block(d, group, last, a, row0, prow, b, gstep0, dst, sdst);
     __syncthreads();
   }
@@ -127,10 +160,16 @@ static hipError_t launch_rows_grouped(const QuantGroupedArgs& a, const Device& d
   return hipGetLastError();
 }
 
+// Rows per pass: two, for the longer runs of codes per store; one above 16384
+// channels (1024 threads), and above 8192 as long as every row is in flight at once (128
+// x 14336 6.2 / 7.1 us with one / two); four up to 2048 channels unless there is little
+// to do (us, 1 / 2 / 4 rows per pass, slots x K: 32 x 1024 4.4 / 4.3 / 4.5, 256 x 1024
+// 4.9 / 4.4 / 4.7, 1024 x 1024 6.0 / 5.4 / 4.9, 8192 x 2048 18.0 / 14.8 / 13.7, 1024 x
+// 4096 7.4 / 6.6 / 7.4, 8192 x 4096 27.5 / 22.4 / 22.0, 8192 x 8192 52 / 46 / 45).
 hipError_t launch_quantize_grouped(const QuantGroupedArgs& a, const Device& dev, hipStream_t stream) {
-  const int64_t n = a.q.rp * a.q.K;
-  int rh = a.q.K <= 8192 ? 4 : (a.q.K <= 16384 ? 2 : 1);
-  if (n < (1 << 20)) rh = 1;
+  int rh = 2;
+  if (a.q.K <= 2048) rh = a.q.rp * a.q.K < (1 << 20) ? 2 : 4;
+  else if (a.q.K > 16384 || (a.q.K > 8192 && a.q.rp <= 2 * dev.cus)) rh = 1;
   switch (rh) {
     case 1: return launch_rows_grouped<1>(a, dev, stream);
     case 2: return launch_rows_grouped<2>(a, dev, stream);

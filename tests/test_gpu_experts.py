@@ -12,6 +12,7 @@ import torch
 
 from oracle import mx_oracle as O
 from tests import expert_cases as C
+from tests import grouped_routes as R
 from tests import packed_layout as L
 from tests.gpu_helpers import assert_gemm_close, note, to_dev_bf16, to_dev_perm, y_to_f64
 
@@ -159,7 +160,8 @@ def test_quantize_grouped_widths(split, formats):
 # ---- the grouped product ----
 
 
-def _grouped(tokens, top_k, experts, N, split, kind, formats=DEFAULT, own_sigma=False, seed=0):
+def _grouped(tokens, top_k, experts, N, split, kind, formats=DEFAULT, own_sigma=False, seed=0, cols=None):
+    """The product's inputs on the GPU, and its reference (of the columns `cols` alone where given)."""
     b, K = _b(), sum(split)
     ids = C.make_ids(tokens * top_k, experts, kind, seed)
     xb, perms = C.activations(tokens, K, experts if own_sigma else 1, seed)
@@ -168,7 +170,7 @@ def _grouped(tokens, top_k, experts, N, split, kind, formats=DEFAULT, own_sigma=
     g = b.group_rows(_dev_ids(ids), experts)
     a = _garbage(b.MXTensor.empty(g.capacity, K, split, formats=formats))
     b.quantize_act_grouped(to_dev_bf16(xb), g, _perm_arg(perms), split, top_k=top_k, out=a)
-    return ids, g, a, w, C.grouped_product(xb, ids, top_k, perms, wb, split, formats)
+    return ids, g, a, w, C.grouped_product(xb, ids, top_k, perms, wb if cols is None else wb[:, cols], split, formats)
 
 
 def _check_rows(y, ref, before, ctx):
@@ -214,6 +216,19 @@ def test_gemm_grouped_long(tokens, top_k, experts, N, split):
     y = _b().gemm_grouped(a, w, g)
     torch.cuda.synchronize()
     _check_rows(y, ref, 0.0, (tokens, N, split))
+
+
+@pytest.mark.parametrize("formats", [("E3M2", "E4M3"), ("E2M3", "E5M2"), ("E3M2", "E5M2"), ("E2M3", "E4M3")], ids="-".join)
+@pytest.mark.parametrize("kernel,slots,experts,N,split", R.CASES, ids=str)
+def test_gemm_grouped_kernels(kernel, slots, experts, N, split, formats):
+    """Every compiled kernel with every format set, at sizes that are no multiple of its tile."""
+    assert R.route(slots, experts, N, split, torch.cuda.get_device_properties(0).multi_processor_count)[0] == kernel
+    note(f"gemm grouped {kernel} {formats}")
+    cols = np.unique(np.concatenate([np.arange(0, N, max(1, N // 200)), np.arange(max(0, N - 40), N)]))
+    ids, g, a, w, ref = _grouped(slots, 1, experts, N, split, "skewed", formats, own_sigma=True, seed=8, cols=cols)
+    y = _b().gemm_grouped(a, w, g)
+    torch.cuda.synchronize()
+    _check_rows(y[:, torch.from_numpy(cols).cuda()], ref, 0.0, (kernel, formats))
 
 
 def test_gemm_grouped_matches_gemm_alone():
