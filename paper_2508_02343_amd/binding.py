@@ -136,6 +136,8 @@ def _load_packed(path: str = LIB_PATH) -> ctypes.CDLL:
 
 _fast = _load_packed()
 
+_BF16, _INT32 = torch.bfloat16, torch.int32
+
 
 class MMError(RuntimeError):
     def __init__(self, status: int, message: str):
@@ -420,18 +422,73 @@ def _here(index: int, name: str) -> None:
         raise ValueError(f"{name} must be on the current device")
 
 
+def _check_rows(x: torch.Tensor) -> int:
+    """bf16 rows on the current device; the device's index."""
+    if x.dtype is not _BF16 or x.dim() != 2 or x.stride(1) != 1 or not x.is_cuda:
+        raise ValueError("x must be a 2-D row-major bfloat16 device tensor")
+    index = x.get_device()
+    _here(index, "x")
+    return index
+
+
 def _check_perms(perm: torch.Tensor, experts: int, K: int, index: int) -> int:
     """One sigma [K] for all experts, or one each [experts, K]; its stride."""
-    if (perm.dtype != torch.int32 or not perm.is_contiguous() or perm.get_device() != index
-            or (tuple(perm.shape) != (K,) and tuple(perm.shape) != (experts, K))):
+    n = perm.dim()
+    if (perm.dtype is not _INT32 or not perm.is_contiguous() or perm.get_device() != index
+            or (perm.shape != (K,) if n == 1 else perm.shape != (experts, K))):
         raise ValueError(f"perm must be a contiguous int32 tensor [{K}] or [{experts}, {K}] on x's device")
-    return 0 if perm.dim() == 1 else K
+    return 0 if n == 1 else K
+
+
+def _packed_checked(t, index: int, name: str, count: int = 1) -> bytes:
+    """The descriptor of an MXTensor, or of an MXStack of `count` operands, whose
+    buffers hold its layout on the device (the library reads and writes exactly
+    those bytes).  (_check_buffers and _packed in one pass over the buffers: half the
+    time.)"""
+    split = t.split
+    if type(split) is not tuple:
+        split = tuple(map(int, split))
+    n4, n6, n8, nsc = _buffer_sizes(t.rows, t.K, split)
+    q4, q6, q8, sc = t.q4, t.q6, t.q8, t.sc
+    p4 = p6 = p8 = 0
+    if q4 is not None:
+        if q4.nbytes < n4 * count or q4.get_device() != index or not q4.is_contiguous():
+            _refuse_buffer(t, index, name, count)
+        p4 = q4.data_ptr()
+    elif n4:
+        _refuse_buffer(t, index, name, count)
+    if q6 is not None:
+        if q6.nbytes < n6 * count or q6.get_device() != index or not q6.is_contiguous():
+            _refuse_buffer(t, index, name, count)
+        p6 = q6.data_ptr()
+    elif n6:
+        _refuse_buffer(t, index, name, count)
+    if q8 is not None:
+        if q8.nbytes < n8 * count or q8.get_device() != index or not q8.is_contiguous():
+            _refuse_buffer(t, index, name, count)
+        p8 = q8.data_ptr()
+    elif n8:
+        _refuse_buffer(t, index, name, count)
+    if sc is None or sc.nbytes < nsc * count or sc.get_device() != index or not sc.is_contiguous():
+        _refuse_buffer(t, index, name, count)
+    f6, f8 = t.formats
+    return _DESC.pack(t.rows, t.K, *split, FP6_FORMATS.get(f6, -1), FP8_FORMATS.get(f8, -1), p4, p6, p8, sc.data_ptr())
+
+
+def _refuse_buffer(t, index: int, name: str, count: int) -> None:
+    """Says which buffer _packed_checked found wrong."""
+    for b, buf, need in zip(("q4", "q6", "q8", "sc"), (t.q4, t.q6, t.q8, t.sc), _buffer_sizes(t.rows, t.K, tuple(map(int, t.split)))):
+        n = 0 if buf is None else buf.nbytes
+        if n < need * count:
+            raise ValueError(f"{name}.{b} holds {n} bytes, the layout of {count} operand{'s' * (count > 1)} needs {need * count}")
+        if buf is not None and (buf.get_device() != index or not buf.is_contiguous()):
+            raise ValueError(f"{name}.{b} must be contiguous and on {'the CPU' if index < 0 else f'cuda:{index}'}")
 
 
 def group_rows(ids: torch.Tensor, experts: int, out: RowGroups | None = None, stream=None) -> RowGroups:
     """mm_group_rows: the slots whose experts `ids` names (int32, any shape, taken in
     order) grouped by expert.  Ids outside [0, experts) are in no group."""
-    if ids.dtype != torch.int32 or not ids.is_contiguous():
+    if ids.dtype is not _INT32 or not ids.is_contiguous():
         raise ValueError("ids must be a contiguous int32 device tensor")
     index = ids.get_device()
     _here(index, "ids")
@@ -449,44 +506,27 @@ def quantize_act_grouped(x: torch.Tensor, groups: RowGroups, perm: torch.Tensor,
     of `groups` (slot s takes row s // top_k), with one sigma [K] or one per expert
     [experts, K].  The result has groups.capacity rows; those without a slot are
     not written."""
-    if x.dtype != torch.bfloat16 or x.dim() != 2 or x.stride(1) != 1 or not x.is_cuda:
-        raise ValueError("x must be a 2-D row-major bfloat16 device tensor")
+    index = _check_rows(x)
     rows, K = x.shape
-    index = x.get_device()
-    _here(index, "x")
     if rows * top_k != groups.rows or groups.device_index != index:
         raise ValueError(f"x has {rows} rows of {top_k} slots each, the groups are of {groups.rows} slots (on x's device)")
     stride = _check_perms(perm, groups.experts, K, index)
-    split = tuple(map(int, split))
+    if type(split) is not tuple:
+        split = tuple(map(int, split))
     if out is None:
         out = MXTensor.empty(groups.capacity, K, split, device=x.device, formats=formats)
-    else:
-        _check_layout(out, groups.capacity, K, split, x.device, "out")
-    _check(_fast.mm_quantize_act_grouped(x.data_ptr(), x.stride(0), top_k, perm.data_ptr(), stride,
-                                         groups._packed(), out._packed(), _stream_int(stream)))
+    elif out.rows != groups.capacity or out.K != K or tuple(out.split) != split:
+        raise ValueError(f"out is [{out.rows}, {out.K}] split {tuple(out.split)}, expected [{groups.capacity}, {K}] split {split}")
+    _check(_fast.mm_quantize_act_grouped(x.data_ptr(), x.stride(0), top_k, perm.data_ptr(), stride, groups._packed(),
+                                         _packed_checked(out, index, "out"), _stream_int(stream)))
     return out
-
-
-def _check_weights(w, index: int, device) -> int:
-    """An MXTensor, or an MXStack (its buffers hold count operands); the number of experts."""
-    if not isinstance(w, MXStack):
-        _check_buffers(w, w.rows, w.K, tuple(map(int, w.split)), device, "w")
-        return 1
-    for b, buf, need in zip(("q4", "q6", "q8", "sc"), (w.q4, w.q6, w.q8, w.sc), _buffer_sizes(w.rows, w.K, w.split)):
-        n = 0 if buf is None else buf.nbytes
-        if n < need * w.count:
-            raise ValueError(f"w.{b} holds {n} bytes, {w.count} experts need {need * w.count}")
-        if buf is not None and (buf.get_device() != index or not buf.is_contiguous()):
-            raise ValueError(f"w.{b} must be contiguous and on {device}")
-    return w.count
 
 
 def _result(y: torch.Tensor | None, M: int, N: int, index: int, device) -> torch.Tensor:
     """A bf16 [M, N] result; a new one is zero, as some of its rows may not be written."""
     if y is None:
         return torch.zeros((M, _round16(N) if N % 8 else N), dtype=torch.bfloat16, device=device)[:, :N]
-    if (y.dtype != torch.bfloat16 or y.dim() != 2 or tuple(y.shape) != (M, N) or y.stride(1) != 1
-            or y.get_device() != index):
+    if y.dtype is not _BF16 or y.shape != (M, N) or y.stride(1) != 1 or y.get_device() != index:
         raise ValueError(f"y must be a bfloat16 [{M}, {N}] tensor with unit column stride on {device}")
     return y
 
@@ -496,16 +536,15 @@ def gemm_grouped(a: MXTensor, w: MXStack, groups: RowGroups, y: torch.Tensor | N
     """mm_gemm_grouped: Y [slots, N], row s the product of slot s's packed row and its
     expert's weight.  Rows of slots in no group are left as they were in `y` (zero
     without it)."""
-    device, index = a.sc.device, a.sc.get_device()
-    _here(index, "a")
-    _check_buffers(a, groups.capacity, a.K, tuple(map(int, a.split)), device, "a")
-    if a.rows != groups.capacity or groups.device_index != index:
-        raise ValueError(f"a has {a.rows} rows, the groups' capacity is {groups.capacity} (on a's device)")
-    if not isinstance(w, MXStack) or _check_weights(w, index, device) != groups.experts:
+    index = groups.device_index
+    _here(index, "groups")
+    if a.rows != groups.capacity:
+        raise ValueError(f"a has {a.rows} rows, the groups' capacity is {groups.capacity}")
+    if not isinstance(w, MXStack) or w.count != groups.experts:
         raise ValueError(f"w must be an MXStack of the groups' {groups.experts} experts")
-    y = _result(y, groups.rows, w.rows, index, device)
-    _check(_fast.mm_gemm_grouped(a._packed(), w._packed(), groups._packed(), y.data_ptr(), y.stride(0),
-                                 _stream_int(stream)))
+    y = _result(y, groups.rows, w.rows, index, groups.map.device)
+    _check(_fast.mm_gemm_grouped(_packed_checked(a, index, "a"), _packed_checked(w, index, "w", w.count),
+                                 groups._packed(), y.data_ptr(), y.stride(0), _stream_int(stream)))
     return y
 
 
@@ -528,30 +567,36 @@ def gemv(x: torch.Tensor, w: MXTensor | MXStack, perm: torch.Tensor, ids: torch.
     weight of w (MXStack); at most 16 rows of Y.  perm as for
     quantize_act_grouped.  Rows whose id names no expert are left as they were in
     `y` (zero without it)."""
-    if x.dtype != torch.bfloat16 or x.dim() != 2 or x.stride(1) != 1 or not x.is_cuda:
-        raise ValueError("x must be a 2-D row-major bfloat16 device tensor")
+    index = _check_rows(x)
     n, K = x.shape
-    device, index = x.device, x.get_device()
-    _here(index, "x")
-    experts = _check_weights(w, index, device)
     if w.K != K:
         raise ValueError(f"x has {K} channels, w {w.K}")
-    if (ids is None) != (not isinstance(w, MXStack)):
-        raise ValueError("ids go with an MXStack, an MXTensor takes none")
     rows = n * top_k
-    if ids is not None and (ids.dtype != torch.int32 or not ids.is_contiguous() or ids.numel() != rows
-                            or ids.get_device() != index):
-        raise ValueError(f"ids must be a contiguous int32 tensor of {rows} elements on x's device")
+    if ids is None:
+        if isinstance(w, MXStack):
+            raise ValueError("an MXStack needs ids")
+        experts, p_ids = 1, 0
+    else:
+        if not isinstance(w, MXStack):
+            raise ValueError("ids go with an MXStack")
+        if ids.dtype is not _INT32 or not ids.is_contiguous() or ids.numel() != rows or ids.get_device() != index:
+            raise ValueError(f"ids must be a contiguous int32 tensor of {rows} elements on x's device")
+        experts, p_ids = w.count, ids.data_ptr()
     stride = _check_perms(perm, experts, K, index)
-    need = gemv_workspace_size(rows, K, w.split)
-    if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-    elif not workspace.is_contiguous() or workspace.get_device() != index:
-        raise ValueError("workspace must be contiguous and on x's device")
-    y = _result(y, rows, w.rows, index, device)
-    _check(_fast.mm_gemv(x.data_ptr(), x.stride(0), rows, top_k, perm.data_ptr(), stride, w._packed(),
-                         experts, 0 if ids is None else ids.data_ptr(), 0 if workspace is None else workspace.data_ptr(),
-                         0 if workspace is None else workspace.nbytes, y.data_ptr(), y.stride(0), _stream_int(stream)))
+    p_ws = n_ws = 0
+    if workspace is not None:
+        if not workspace.is_contiguous() or workspace.get_device() != index:
+            raise ValueError("workspace must be contiguous and on x's device")
+        p_ws, n_ws = workspace.data_ptr(), workspace.nbytes
+    else:
+        n_ws = gemv_workspace_size(rows, K, w.split) if type(w.split) is not tuple else _gemv_workspace(rows, K, w.split)
+        if n_ws:
+            workspace = torch.empty(n_ws, dtype=torch.uint8, device=x.device)
+            p_ws = workspace.data_ptr()
+    y = _result(y, rows, w.rows, index, x.device)
+    _check(_fast.mm_gemv(x.data_ptr(), x.stride(0), rows, top_k, perm.data_ptr(), stride,
+                         _packed_checked(w, index, "w", experts), experts, p_ids, p_ws, n_ws, y.data_ptr(), y.stride(0),
+                         _stream_int(stream)))
     return y
 
 

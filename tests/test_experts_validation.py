@@ -203,10 +203,17 @@ def test_sigma_and_result_checks():
         with pytest.raises(ValueError):
             b._check_perms(bad, 4, K, -1)
     w = b.MXStack.empty(4, 16, K, SPLIT, device="cpu")
-    assert b._check_weights(w, -1, torch.device("cpu")) == 4 and b._check_weights(w[0], -1, torch.device("cpu")) == 1
-    w.q8 = w.q8[:-1]
-    with pytest.raises(ValueError, match=r"w\.q8"):
-        b._check_weights(w, -1, torch.device("cpu"))
+    for t, count in ((w, 4), (w[0], 1)):
+        assert b._packed_checked(t, -1, "w", count) == t._packed()
+    for name in ("q4", "q6", "q8", "sc"):
+        full = getattr(w, name)
+        for bad in (full[:-1], torch.cat([full, full])[::2], None):
+            setattr(w, name, bad)
+            with pytest.raises(ValueError, match=rf"w\.{name}"):
+                b._packed_checked(w, -1, "w", 4)
+        setattr(w, name, full)
+    with pytest.raises(ValueError, match=r"w\.q4 must be contiguous and on cuda:3"):
+        b._packed_checked(w, 3, "w", 4)
     y = torch.zeros(40, 16, dtype=torch.bfloat16)
     assert b._result(y, 40, 16, -1, y.device) is y
     for bad in (y[:39], y.float(), y.T, y[:, :15]):
