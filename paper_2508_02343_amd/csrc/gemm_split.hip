@@ -465,8 +465,8 @@ hipError_t launch_gemm_split(const GemmArgs& a, int shape, const Device& dev, hi
 template <int I, int FS>
 static hipError_t launch_grouped_fs(const GemmGroupedArgs& a, const Device& dev, hipStream_t stream) {
   constexpr int TN = kSplitShapes[I].tn, TM = kSplitShapes[I].tm;
-  constexpr int kList = TM == 1 ? 0 : 2;
-  static_assert(TM == 1 << kList, "a listed tile size");
+  constexpr int kList = TM == 1 ? 0 : 1;
+  static_assert(32 * TM == kTileRows[kList], "a listed tile size");
   constexpr int lds = lds_bytes<TN, TM>();
   static DeviceOnce once;
   hipError_t e = allow_lds(once, dev, reinterpret_cast<const void*>(gemm_split_grouped_kernel<TN, TM, FS>), lds);

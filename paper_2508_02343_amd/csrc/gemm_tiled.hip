@@ -850,8 +850,8 @@ static hipError_t launch_plain(const GemmArgs& g, const Device& dev, hipStream_t
 
 template <int BN, int BM>
 static hipError_t launch_grouped(const GemmGroupedArgs& g, const Device& dev, hipStream_t stream) {
-  constexpr int kList = BM == 128 ? 2 : 3;
-  static_assert(BM == kRowGroup << kList, "a listed tile size");
+  constexpr int kList = BM == 128 ? 1 : 2;
+  static_assert(BM == kTileRows[kList], "a listed tile size");
   const Grouped a = {g, (int)((g.g.w.rows + BN - 1) / BN), g.tiles[kList], g.counts + kList};
   return launch_tile<BN, BM>(a, g.g.fs, (int64_t)a.tiles_n * g.ntiles[kList], dev, stream);
 }

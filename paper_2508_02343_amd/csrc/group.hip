@@ -11,6 +11,11 @@
 // front and the padded starts give every wavefront its first row of each expert.
 // More than kGroupChunk slots: a first launch leaves each workgroup's counts, the
 // second places.
+//
+// Measured (us, as graph replays): 16 slots of 8 experts 6.5, 65536 of 128 11.7 (two
+// launches; 0.05 TB/s of ids and rows).  What it takes is its chain of steps: the
+// ids' load, a ballot per bit, four barriers, the stores.  With 4096 slots per
+// workgroup and the ids read twice instead of kept with their ranks, 21.5.
 #include "grouped.hpp"
 
 namespace mm {
@@ -81,9 +86,10 @@ __global__ __launch_bounds__(kThreads) void group_place_kernel(GroupArgs a, int 
   uint32_t* const next = lds;                            // [kWaves][E]
   int* const total = (int*)(lds + kWaves * E);           // [E] slots of each expert
   int* const front = total + E;                          // [E] those of the workgroups in front
-  int* const start = front + E;                          // [E + 1] first row group
-  int* const tile0 = start + E + 1;                      // [3][E] first tile of 2, 4, 8 row groups
-  int (*const part)[kTileLists] = (int (*)[kTileLists])(tile0 + 3 * E);  // [kWaves]
+  int* const start = front + E;                          // [E] first row group
+  int* const tile0 = start + E;                          // [2][E] first tile of 128 and of 256 rows
+  int (*const part)[kTileLists] = (int (*)[kTileLists])(tile0 + 2 * E);  // [kWaves]
+  __shared__ int ends[kTileLists];  // tiles in all
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t run = ((int64_t)blockIdx.x * kWaves + wave) * 64 * a.turns;
   int key[kTurns], rank[kTurns];
@@ -139,28 +145,30 @@ __global__ __launch_bounds__(kThreads) void group_place_kernel(GroupArgs a, int 
     before = front[e];
     all = a.blocks > 1 ? total[e] : here;
   }
-  const int g = (all + kRowGroup - 1) / kRowGroup;
-  int v[kTileLists] = {g, (g + 1) / 2, (g + 3) / 4, (g + 7) / 8};
-  const int own[kTileLists] = {v[0], v[1], v[2], v[3]};
+  int v[kTileLists];
+#pragma unroll
+  for (int k = 0; k < kTileLists; ++k) v[k] = (all + kTileRows[k] - 1) / kTileRows[k];
+  const int own[kTileLists] = {v[0], v[1], v[2]};
   scan<kTileLists>(v, part, lane, wave);
+  if (threadIdx.x == kThreads - 1)
+#pragma unroll
+    for (int k = 0; k < kTileLists; ++k) ends[k] = v[k];
   if (e < E) {
     const int s = v[0] - own[0];
     start[e] = s;
     total[e] = all;
 #pragma unroll
     for (int k = 1; k < kTileLists; ++k) tile0[(k - 1) * E + e] = v[k] - own[k];
-    if (e == E - 1) {
-      start[E] = v[0];
-      if (blockIdx.x == 0) {
-        a.starts[E] = v[0] * kRowGroup;
-#pragma unroll
-        for (int k = 0; k < kTileLists; ++k) a.tile_counts[k] = v[k];
-      }
-    }
     if (blockIdx.x == 0) a.starts[e] = s * kRowGroup;
     for (int w = 0; w < kWaves; ++w) next[w * E + e] += (uint32_t)(s * kRowGroup + before);
   }
   __syncthreads();
+  const int used = ends[0];  // row groups
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    a.starts[E] = used * kRowGroup;
+#pragma unroll
+    for (int k = 0; k < kTileLists; ++k) a.tile_counts[k] = ends[k];
+  }
   // the slots, in their order
   if (kept) {
 #pragma unroll
@@ -179,7 +187,6 @@ __global__ __launch_bounds__(kThreads) void group_place_kernel(GroupArgs a, int 
     }
   }
   // the row groups: owner, rows without a slot, tiles
-  const int used = start[E];
   const int at = blockIdx.x * kThreads + threadIdx.x, stride = a.blocks * kThreads;
   for (int q = at; q < a.groups; q += stride) {
     int owner = -1, filled = 0;
@@ -191,35 +198,30 @@ __global__ __launch_bounds__(kThreads) void group_place_kernel(GroupArgs a, int 
         else hi = mid;
       }
       owner = lo;
-      const int rel = q - start[lo], left = total[lo] - rel * kRowGroup;
-      filled = left < kRowGroup ? left : kRowGroup;
-      const uint32_t o = (uint32_t)owner;
-      a.tiles[0][q] = RowTile{q, o | (uint32_t)filled << 16};
+      const int rel = q - start[lo], rest = total[lo] - rel * kRowGroup;
+      filled = rest < kRowGroup ? rest : kRowGroup;
 #pragma unroll
-      for (int k = 1; k < kTileLists; ++k)
-        if ((rel & ((1 << k) - 1)) == 0) {
-          const int most = kRowGroup << k;
-          a.tiles[k][tile0[(k - 1) * E + lo] + (rel >> k)] = RowTile{q, o | (uint32_t)(left < most ? left : most) << 16};
-        }
-    } else {
-      a.tiles[0][q] = RowTile{-1, 0};
+      for (int k = 0; k < kTileLists; ++k) {
+        const int rows = kTileRows[k], per = rows / kRowGroup;
+        if (rel % per == 0)
+          a.tiles[k][k == 0 ? q : tile0[(k - 1) * E + lo] + rel / per] =
+              RowTile{q, (uint32_t)owner | (uint32_t)(rest < rows ? rest : rows) << 16};
+      }
     }
     a.owners[q] = owner;
     for (int r = filled; r < kRowGroup; ++r) a.slots[(int64_t)q * kRowGroup + r] = -1;
   }
-  // tiles behind the last
+  // places behind the last tile
 #pragma unroll
-  for (int k = 1; k < kTileLists; ++k) {
-      const int n = tile0[(k - 1) * E + E - 1] + ((start[E] - start[E - 1] + (1 << k) - 1) >> k);
-    for (int i = n + at; i < a.ntiles[k]; i += stride) a.tiles[k][i] = RowTile{-1, 0};
-  }
+  for (int k = 0; k < kTileLists; ++k)
+    for (int i = ends[k] + at; i < a.ntiles[k]; i += stride) a.tiles[k][i] = RowTile{-1, 0};
 }
 
 hipError_t launch_group_rows(const GroupArgs& a, const Device& dev, hipStream_t stream) {
   int bits = 1;
   while ((1 << bits) <= a.experts) ++bits;  // keys 0 .. experts
   const int E = a.experts;
-  auto place_lds = [](int n) { return ((kWaves + 6) * n + 1 + kWaves * kTileLists) * 4; };
+  auto place_lds = [](int n) { return ((kWaves + 5) * n + kWaves * kTileLists) * 4; };
   static DeviceOnce once;
   hipError_t e = allow_lds(once, dev, reinterpret_cast<const void*>(group_place_kernel), place_lds(kMaxExperts));
   if (e != hipSuccess) return e;

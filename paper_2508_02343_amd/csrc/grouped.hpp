@@ -17,8 +17,9 @@ struct RowTile {
   uint32_t owner_rows;
 };
 
-// Tiles of 1, 2, 4 and 8 row groups (32, 64, 128, 256 rows) are listed.
-constexpr int kTileLists = 4;
+// Tiles of these many rows are listed.
+constexpr int kTileLists = 3;
+constexpr int kTileRows[kTileLists] = {32, 128, 256};
 
 // group_rows: one workgroup of 1024 threads up to kGroupChunk slots, above one for
 // every 1024 slots, at most kGroupMaxBlocks.
@@ -48,15 +49,16 @@ inline GroupLayout group_layout(int64_t rows, int64_t experts) {
   int64_t at = l.owners + round4(groups);
   for (int k = 0; k < kTileLists; ++k) {
     l.tiles[k] = at;
-    // sum over experts of ceil(groups / 2^k): no more than this, and than the groups
-    const int64_t n = (groups >> k) + most;
+    // sum over experts of ceil(their groups / groups per tile): no more than this,
+    // and than the groups
+    const int64_t n = groups / (kTileRows[k] / kRowGroup) + most;
     l.ntiles[k] = n < groups ? n : groups;
     at += round4(2 * l.ntiles[k]);
   }
   const int64_t b = rows <= kGroupChunk ? 1 : (rows + kGroupThreads - 1) / kGroupThreads;
   l.blocks = b > kGroupMaxBlocks ? kGroupMaxBlocks : b;
   l.tile_counts = at;
-  at += kTileLists;
+  at += round4(kTileLists);
   l.counts = at;
   if (l.blocks > 1) at += round4(l.blocks * experts);
   l.words = at;

@@ -15,7 +15,7 @@ struct GroupedSizes {
   int64_t slots, experts, n;  // n: weight rows of an expert
   int steps[3];
   int cus;
-  int64_t ntiles[4];          // tile lists' lengths: 32, 64, 128, 256 rows
+  int64_t ntiles[3];          // tile lists' lengths: 32, 128, 256 rows
 };
 
 // Estimates in us: per call, per round of tiles over the CUs (at least one), per
@@ -40,9 +40,9 @@ struct GroupedChoice {
 constexpr GroupedChoice kGroupedChoices[] = {
     {GemmKernel::kSplit, 0, 1, 1, 0, 512, {3.26, 0, 0.0421, 0.0594, 0.840}},
     {GemmKernel::kSplit, 1, 2, 1, 0, 512, {3.20, 0.243, 0.0494, 0.0849, 0.670}},
-    {GemmKernel::kSplit, 4, 2, 4, 2, 512, {3.23, 2.13, 0.0852, 0.0746, 0.903}},
-    {GemmKernel::kTiled128, 0, 8, 4, 2, 512, {3.64, 2.57, 0.278, 0.0646, 0.343}},
-    {GemmKernel::kTiled256, 0, 8, 8, 3, 256, {5.12, 5.21, 0.459, 0.0592, 0.411}},
+    {GemmKernel::kSplit, 4, 2, 4, 1, 512, {3.23, 2.13, 0.0852, 0.0746, 0.903}},
+    {GemmKernel::kTiled128, 0, 8, 4, 1, 512, {3.64, 2.57, 0.278, 0.0646, 0.343}},
+    {GemmKernel::kTiled256, 0, 8, 8, 2, 256, {5.12, 5.21, 0.459, 0.0592, 0.411}},
 };
 
 // shape -1: no kernel's grid takes the sizes.

@@ -16,13 +16,13 @@ MAIN = """
 #include "%s"
 int main() {
   mm::GroupedSizes z;
-  long long v[7];
-  while (scanf("%%lld %%lld %%lld %%d %%d %%d %%d %%lld %%lld %%lld %%lld", v, v + 1, v + 2, &z.steps[0], &z.steps[1],
-               &z.steps[2], &z.cus, v + 3, v + 4, v + 5, v + 6) == 11) {
+  long long v[6];
+  while (scanf("%%lld %%lld %%lld %%d %%d %%d %%d %%lld %%lld %%lld", v, v + 1, v + 2, &z.steps[0], &z.steps[1],
+               &z.steps[2], &z.cus, v + 3, v + 4, v + 5) == 10) {
     z.slots = v[0], z.experts = v[1], z.n = v[2];
-    for (int k = 0; k < 4; ++k) z.ntiles[k] = v[3 + k];
+    for (int k = 0; k < 3; ++k) z.ntiles[k] = v[3 + k];
     const mm::GemmRoute r = mm::grouped_route(z);
-    int tn = 8, tm = r.kernel == mm::GemmKernel::kTiled256 ? 8 : 4, list = tm == 8 ? 3 : 2;
+    int tn = 8, tm = r.kernel == mm::GemmKernel::kTiled256 ? 8 : 4, list = tm == 8 ? 2 : 1;
     if (r.shape < 0) {
       puts("none 0 0");
       continue;
@@ -30,7 +30,7 @@ int main() {
     if (r.kernel == mm::GemmKernel::kSplit) {
       tn = mm::kSplitShapes[r.shape].tn;
       tm = mm::kSplitShapes[r.shape].tm;
-      list = tm == 1 ? 0 : 2;
+      list = tm == 1 ? 0 : 1;
     }
     printf("%%s%%dx%%d %%lld %%d\\n", r.kernel == mm::GemmKernel::kSplit ? "split" : "tiled", 32 * tn, 32 * tm,
            (long long)(mm::ceil_div(z.n, 32 * tn) * z.ntiles[list]), tm == 8 ? 256 : 512);
@@ -53,7 +53,7 @@ def route(slots: int, experts: int, N: int, split, cus: int = 256) -> tuple[str,
     """(kernel and tile, tiles in the grid, threads of a workgroup)."""
     most = min(experts, slots)
     groups = (slots + 31 * most) // 32
-    ntiles = [min((groups >> k) + most, groups) for k in range(4)]
+    ntiles = [min(groups // k + most, groups) for k in (1, 4, 8)]
     steps = [-(-(p // 32) // 4) for p in split]
     line = " ".join(str(v) for v in (slots, experts, N, *steps, cus, *ntiles))
     out = subprocess.run([_program()], input=line, check=True, capture_output=True, text=True).stdout.split()
