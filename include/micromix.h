@@ -347,7 +347,9 @@ mm_status mm_group_rows(const int32_t* ids, const mm_row_groups* out, void* stre
  *   perm     device, int32, 16-byte aligned: sigma of expert e at perm + e *
  *            perm_stride, perm_stride 0 (one sigma for all experts) or at least K
  *            and a multiple of 4.
- *   groups   a map that mm_group_rows filled, on this stream or before it.
+ *   groups   a map that mm_group_rows filled, on this stream or before it (with
+ *            another content of the map the results are unspecified, but the
+ *            grouped calls stay in bounds).
  *   out      descriptor with rows = the map's capacity.
  * K may be at most 32768.  Errors: those of mm_quantize_act, MM_ERR_VALUE.
  */
@@ -390,7 +392,8 @@ mm_status mm_gemv_workspace_size(int64_t rows, int64_t K, mm_split split, int64_
  *   rows        rows of Y, 1 .. 16 (more: mm_quantize_act and mm_gemm).
  *   top_k       1 .. 16, rows of Y per row of x.
  *   perm, perm_stride  as for mm_quantize_act_grouped.
- *   w, experts  as for mm_gemm_grouped (experts 1 .. 1024).
+ *   w, experts  as for mm_gemm_grouped (experts 1 .. 1024); K at most 32768, N at
+ *               most 2^28.
  *   ids         device, int32 [rows], 4-byte aligned, any values; NULL: every row
  *               takes the first weight.
  *   workspace   device, caller-owned, 16-byte aligned, at least

@@ -348,7 +348,7 @@ def _group_sizes(rows: int, experts: int) -> tuple:
     return sz.capacity, sz.slots, sz.owners, sz.bytes
 
 
-@dataclass
+@dataclass(frozen=True, eq=False)
 class RowGroups:
     """Row-group map in device memory (include/micromix.h): `rows` slots in order
     of their experts.  starts [experts + 1], slots [capacity] and owners
@@ -359,14 +359,13 @@ class RowGroups:
     map: torch.Tensor
 
     def __post_init__(self):
-        self.capacity, slots, owners, nbytes = _group_sizes(int(self.rows), int(self.experts))
+        capacity, slots, owners, nbytes = _group_sizes(int(self.rows), int(self.experts))
         m = self.map
         if m.dtype != torch.int32 or m.dim() != 1 or not m.is_contiguous() or m.nbytes < nbytes:
             raise ValueError(f"map must be a contiguous int32 tensor of at least {nbytes // 4} words")
-        self.starts = m[:self.experts + 1]
-        self.slots = m[slots:slots + self.capacity]
-        self.owners = m[owners:owners + self.capacity // 32]
-        self.device_index = m.get_device()
+        for name, value in (("capacity", capacity), ("starts", m[:self.experts + 1]), ("slots", m[slots:slots + capacity]),
+                            ("owners", m[owners:owners + capacity // 32]), ("device_index", m.get_device())):
+            object.__setattr__(self, name, value)
 
     @classmethod
     def empty(cls, rows: int, experts: int, device="cuda") -> "RowGroups":

@@ -506,6 +506,7 @@ mm_status mm_quantize_act_grouped(const void* x_bf16, int64_t ldx, int64_t top_k
   a.slots = groups->map + gl.slots;
   a.tiles = tile_list(groups, gl, 0);
   a.experts = (int)groups->experts;
+  a.rows = (uint32_t)groups->rows;
   mm::Device dev;
   hipError_t e = mm::current_device(&dev);
   if (e == hipSuccess) e = mm::launch_quantize_grouped(a, dev, static_cast<hipStream_t>(stream));
@@ -555,6 +556,7 @@ mm_status mm_gemv_workspace_size(int64_t rows, int64_t K, mm_split split, int64_
   if (st != MM_OK) return st;
   st = check_shape(rows, K, split, who);
   if (st != MM_OK) return st;
+  if (K > kMaxQuantK) return fail(MM_ERR_SHAPE, "%s: K=%lld exceeds %lld", who, (long long)K, (long long)kMaxQuantK);
   *bytes = mm::gemv_workspace_bytes(rows, K, layout(rows, split).steps);
   return MM_OK;
 }
@@ -571,6 +573,9 @@ mm_status mm_gemv(const void* x_bf16, int64_t ldx, int64_t rows, int64_t top_k, 
   if (st != MM_OK) return st;
   st = check_tensor(w, "w");
   if (st != MM_OK) return st;
+  if (w->K > kMaxQuantK) return fail(MM_ERR_SHAPE, "%s: K=%lld exceeds %lld", who, (long long)w->K, (long long)kMaxQuantK);
+  if (w->rows > mm::kGemvMaxN)
+    return fail(MM_ERR_SHAPE, "%s: N=%lld exceeds %lld", who, (long long)w->rows, (long long)mm::kGemvMaxN);
   st = check_perms(perm, perm_stride, w->K, who);
   if (st != MM_OK) return st;
   if (top_k <= 0 || top_k > mm::kGemvMaxRows) return fail(MM_ERR_VALUE, "%s: top_k=%lld out of range", who, (long long)top_k);

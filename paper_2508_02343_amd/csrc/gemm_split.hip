@@ -293,8 +293,13 @@ struct RowsInPlace {
 };
 struct RowsBySlot {
   const int32_t* slots;
-  int64_t m_own, M;  // M: behind the tile's rows that hold a slot
-  __device__ __forceinline__ int64_t operator()(int64_t m) const { return m >= M ? -1 : slots[m]; }
+  int64_t M;     // behind the tile's rows that hold a slot
+  int64_t rows;  // of y
+  __device__ __forceinline__ int64_t operator()(int64_t m) const {
+    if (m >= M) return -1;
+    const int32_t s = slots[m];
+    return s < rows ? s : -1;
+  }
 };
 
 // One tile: weight rows n0 .. (those from n_own on are its own), activation rows
@@ -406,16 +411,17 @@ __global__ __launch_bounds__(kThreads) void gemm_split_grouped_kernel(GemmGroupe
   const int id = tile_of(tiles_n * tiles_m);
   const int tn = id / tiles_m, tm = id - tn * tiles_m;
   const RowTile t = tiles[tm];
-  if (t.first < 0) return;  // uniform
-  const int64_t e = t.owner_rows & 0xFFFF;
-  const int n = (int)(t.owner_rows >> 16);
+  const TileRows r = tile_rows(t, 32 * TM, a.g.x.rp, a.experts);
+  const int n = r.rows;
+  if (n == 0) return;  // uniform
+  const int64_t e = r.expert;
   GemmArgs g = a.g;
 #pragma unroll
   for (int k = 0; k < 3; ++k) g.w.q[k] += e * a.next.q[k];
   g.w.sc += e * a.next.sc;
   const int64_t n_own = (int64_t)tn * (32 * TN), m0 = (int64_t)t.first * kRowGroup;
   const int64_t n0 = n_own + 32 * TN <= g.w.rp ? n_own : g.w.rp - 32 * TN;
-  tile_product<TN, TM, FS>(g, lds, n0, n_own, m0, w0, w1, w2, FirstRows{n}, RowsBySlot{a.slots, m0, m0 + n});
+  tile_product<TN, TM, FS>(g, lds, n0, n_own, m0, w0, w1, w2, FirstRows{n}, RowsBySlot{a.slots, m0 + n, a.rows});
 }
 
 template <int TN, int TM, int FS>

@@ -647,7 +647,8 @@ struct Grouped {
   GemmGroupedArgs g;
   int tiles_n;
   const RowTile* tiles;
-  const int32_t* count;  // activation tiles that there are: only the device knows
+  int tiles_m;           // activation tiles that there may be
+  const int32_t* count;  // and that there are: only the device knows
 };
 
 // Args: Plain or Grouped (the grid covers as many tiles as there may be; the
@@ -662,6 +663,7 @@ __global__ __launch_bounds__((Tile<BN, BM>::kThreads), 1) void gemm_tiled_kernel
   int tiles_m;
   if constexpr (kGrouped) {
     tiles_m = *args.count;
+    tiles_m = tiles_m < args.tiles_m ? tiles_m : args.tiles_m;
     if ((int)blockIdx.x >= tiles_n * tiles_m) return;  // uniform
     a = args.g.g;
   } else {
@@ -690,12 +692,14 @@ __global__ __launch_bounds__((Tile<BN, BM>::kThreads), 1) void gemm_tiled_kernel
   int filled = 0;           // grouped: rows of the tile that hold a slot
   if constexpr (kGrouped) {
     const RowTile t = args.tiles[tm];
-    const int64_t e = t.owner_rows & 0xFFFF;
+    const TileRows r = tile_rows(t, BM, a.x.rp, args.g.experts);
+    filled = r.rows;
+    if (filled == 0) return;  // uniform
+    const int64_t e = r.expert;
 #pragma unroll
     for (int k = 0; k < 3; ++k) a.w.q[k] += e * args.g.next.q[k];
     a.w.sc += e * args.g.next.sc;
     m0 = (int64_t)t.first * kRowGroup;
-    filled = (int)(t.owner_rows >> 16);
     x_rows = m0 + (filled + kRowGroup - 1) / kRowGroup * kRowGroup;
   }
 
@@ -778,6 +782,13 @@ __global__ __launch_bounds__((Tile<BN, BM>::kThreads), 1) void gemm_tiled_kernel
   constexpr int kRowStride = BN * 2 + 16;
   static_assert(BM * kRowStride <= kLdsBytes, "epilogue tile fits LDS");
   const int r = c.lane & 31, g = c.lane >> 5;
+  // grouped: the rows' slots, behind the tile in LDS (-1: none); loaded while the
+  // accumulators are rounded, as a load in front of every store would hold it back
+  constexpr int kSlotsOff = BM * kRowStride;
+  static_assert(kSlotsOff + BM * 4 <= kLdsBytes && BM <= T::kThreads, "a slot per row");
+  int32_t slot = -1;
+  if constexpr (kGrouped)
+    if ((int)threadIdx.x < filled) slot = args.g.slots[m0 + threadIdx.x];
   if (!producer) {
 #pragma unroll
     for (int i = 0; i < T::TN; ++i)
@@ -795,6 +806,10 @@ __global__ __launch_bounds__((Tile<BN, BM>::kThreads), 1) void gemm_tiled_kernel
         __builtin_amdgcn_sched_barrier(0);
       }
   }
+  if constexpr (kGrouped)
+    if ((int)threadIdx.x < BM)
+      *reinterpret_cast<__attribute__((address_space(3))) int32_t*>((uintptr_t)(c.lds0 + kSlotsOff + 4 * threadIdx.x)) =
+          slot < args.g.rows ? slot : -1;
   __syncthreads();
   constexpr int kChunks = BN / 8;  // 16-byte chunks per row
   const int64_t M = a.x.rows, N = a.w.rows;
@@ -802,9 +817,8 @@ __global__ __launch_bounds__((Tile<BN, BM>::kThreads), 1) void gemm_tiled_kernel
     const int rr = ch / kChunks, col = (ch - rr * kChunks) * 8;
     int64_t m = m0 + rr;
     const int64_t n = n0 + col;
-    if (kGrouped ? rr >= filled : m >= M) continue;
-    if (n >= N) continue;
-    if constexpr (kGrouped) m = args.g.slots[m];
+    if constexpr (kGrouped) m = lds_read<int32_t>(c.lds0 + kSlotsOff + 4 * rr);
+    if ((kGrouped ? m < 0 : m >= M) || n >= N) continue;
     const u32x4 v = lds_read<u32x4>(c.lds0 + rr * kRowStride + col * 2);
     uint16_t* dst = a.y + m * a.ldy + n;
     if (n + 8 <= N) {
@@ -852,7 +866,7 @@ template <int BN, int BM>
 static hipError_t launch_grouped(const GemmGroupedArgs& g, const Device& dev, hipStream_t stream) {
   constexpr int kList = BM == 128 ? 1 : 2;
   static_assert(BM == kTileRows[kList], "a listed tile size");
-  const Grouped a = {g, (int)((g.g.w.rows + BN - 1) / BN), g.tiles[kList], g.counts + kList};
+  const Grouped a = {g, (int)((g.g.w.rows + BN - 1) / BN), g.tiles[kList], g.ntiles[kList], g.counts + kList};
   return launch_tile<BN, BM>(a, g.g.fs, (int64_t)a.tiles_n * g.ntiles[kList], dev, stream);
 }
 

@@ -17,6 +17,19 @@ struct RowTile {
   uint32_t owner_rows;
 };
 
+// A tile's expert and rows.  A map that mm_group_rows did not fill holds anything: a
+// tile that is not one (no rows, or outside of what the map and the weights hold) is
+// passed over, so that the calls stay in bounds.
+struct TileRows {
+  int expert, rows;
+};
+__device__ __forceinline__ TileRows tile_rows(const RowTile& t, int most, int64_t capacity, int experts) {
+  const TileRows r = {(int)(t.owner_rows & 0xFFFF), (int)(t.owner_rows >> 16)};
+  const bool is = t.first >= 0 && r.rows > 0 && r.rows <= most && r.expert < experts &&
+                  (int64_t)t.first * kRowGroup + r.rows <= capacity;
+  return is ? r : TileRows{0, 0};
+}
+
 // Tiles of these many rows are listed.
 constexpr int kTileLists = 3;
 constexpr int kTileRows[kTileLists] = {32, 128, 256};
@@ -87,6 +100,7 @@ struct QuantGroupedArgs {
   const int32_t *starts, *slots;
   const RowTile* tiles;  // of one row group
   int experts;
+  uint32_t rows;         // slots
 };
 hipError_t launch_quantize_grouped(const QuantGroupedArgs& a, const Device& dev, hipStream_t stream);
 
@@ -111,6 +125,7 @@ hipError_t launch_gemm_split_grouped(const GemmGroupedArgs& a, int shape, const 
 
 // At most this many rows in a call of the matrix-vector kernel.
 constexpr int kGemvMaxRows = 16;
+constexpr int64_t kGemvMaxN = (int64_t)1 << 28;  // (a launch has fewer than 2^32 threads)
 
 struct GemvArgs {
   const uint16_t* x;

@@ -41,7 +41,8 @@ __global__ __launch_bounds__(kMaxQuantThreads) void quantize_grouped_kernel(Quan
   // this workgroup's passes: those of quantize.hip (each XCD a contiguous range, its
   // workgroups in turn), as far as they have rows
   constexpr int kPasses = kRowGroup / RH;  // per row group
-  const int64_t passes = ga.starts[ga.experts] / RH;  // (a multiple of 32 rows)
+  const int64_t used = ga.starts[ga.experts];  // (a multiple of 32 rows)
+  const int64_t passes = (used < a.rp ? used : a.rp) / RH;
   int64_t q, q_end, stride;
   if (gridDim.x % 8 == 0) {
     const int x = blockIdx.x & 7;
@@ -55,11 +56,11 @@ __global__ __launch_bounds__(kMaxQuantThreads) void quantize_grouped_kernel(Quan
   }
   // Moves q on to a pass with rows, and its row group's tile; an expert's rows come
   // first in its row groups.
-  RowTile tile = {};
+  TileRows tile = {};
   auto seek = [&] {  // uniform over the workgroup
     for (; q < q_end; q += stride) {
-      tile = ga.tiles[q / kPasses];
-      if ((int)(q % kPasses) * RH < (int)(tile.owner_rows >> 16)) return;
+      tile = tile_rows(ga.tiles[q / kPasses], kRowGroup, a.rp, ga.experts);
+      if ((int)(q % kPasses) * RH < tile.rows) return;
     }
   };
   constexpr int kParts = 4 / RH;  // a row's 16-byte chunks over the threads: kParts each
@@ -67,9 +68,9 @@ __global__ __launch_bounds__(kMaxQuantThreads) void quantize_grouped_kernel(Quan
   auto load = [&] {
 #pragma unroll
     for (int j = 0; j < RH; ++j) {
-      int32_t s = ga.slots[q * RH + j];
-      s = s < 0 ? ga.slots[q * RH] : s;  // (rows without a slot: the pass's first again)
-      const int64_t row = (uint32_t)s / ga.top_k;
+      uint32_t s = (uint32_t)ga.slots[q * RH + j];
+      if (s >= ga.rows) s = (uint32_t)ga.slots[q * RH];  // (rows without a slot: the pass's first again)
+      const int64_t row = (s < ga.rows ? s : 0) / ga.top_k;
 #pragma unroll
       for (int k = 0; k < kParts; ++k) {
         const uint8_t* src = reinterpret_cast<const uint8_t*>(a.x + row * a.ldx + k * n_act * 8);
@@ -94,8 +95,8 @@ __global__ __launch_bounds__(kMaxQuantThreads) void quantize_grouped_kernel(Quan
   int owner = -1;
   while (q < q_end) {
     const int64_t row0 = q * RH;
-    const int e = (int)(tile.owner_rows & 0xFFFF);
-    const bool filled = (int)(q % kPasses) * RH + prow < (int)(tile.owner_rows >> 16);
+    const int e = tile.expert;
+    const bool filled = (int)(q % kPasses) * RH + prow < tile.rows;
     if (active)
 #pragma unroll
       for (int j = 0; j < 4; ++j)

@@ -129,7 +129,8 @@ def _gemv(x=FAKE, ldx=K, rows=4, top_k=2, perm=FAKE, stride=0, w=None, experts=4
     ({"stride": K - 4}, "MM_ERR_SHAPE"), ({"stride": K + 1}, "MM_ERR_ALIGN"), ({"perm": FAKE + 8}, "MM_ERR_ALIGN"),
     ({"ldy": 15}, "MM_ERR_SHAPE"), ({"ldy": 17}, "MM_ERR_ALIGN"), ({"y": FAKE + 2}, "MM_ERR_ALIGN"),
     ({"w": _tensor(16, (64, 32, 16))}, "MM_ERR_SHAPE"), ({"w": _tensor(16, (64, 48, 16))}, "MM_ERR_SPLIT"),
-    ({"ws": FAKE + 4}, "MM_ERR_ALIGN")])
+    ({"ws": FAKE + 4}, "MM_ERR_ALIGN"), ({"w": _tensor(16, (32768, 32, 0)), "ldx": 32800}, "MM_ERR_SHAPE"),
+    ({"w": _tensor(2**28 + 1), "ldy": 2**28 + 8}, "MM_ERR_SHAPE")])
 def test_gemv_refused(kw, status):
     assert _gemv(**kw) == status
 
@@ -179,6 +180,8 @@ def test_groups_views_and_refusals():
         b.RowGroups(40, 4, g.map.float())
     with pytest.raises(b.MMError, match="MM_ERR_SHAPE"):
         b.RowGroups.empty(0, 4, device="cpu")
+    with pytest.raises(AttributeError):  # the views go with the map
+        g.map = g.map.clone()
 
 
 def test_host_tensors_refused():

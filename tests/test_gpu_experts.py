@@ -249,6 +249,28 @@ def test_gemm_grouped_matches_gemm_alone():
     assert_gemm_close(y_to_f64(alone), ref, "alone")
 
 
+@pytest.mark.parametrize("word", [0, -1, 7, 0x00200005], ids=hex)
+@pytest.mark.parametrize("tokens", [3, 900])
+def test_map_that_was_not_filled(tokens, word):
+    """A map that holds something else: nothing outside the buffers is touched (the rows between the results' columns,
+    and the other operands, stay as they are)."""
+    note(f"map of {word:#x}, {tokens} tokens")
+    b, split, N, E = _b(), (96, 64, 64), 70, 3
+    K = sum(split)
+    xb, perms = C.activations(tokens, K, E, seed=61)
+    w = _stack(C.weights(E, N, K, seed=62), perms, split)
+    before = w.q4.clone()
+    g = b.RowGroups.empty(tokens, E)
+    g.map.fill_(word)
+    a = _garbage(b.MXTensor.empty(g.capacity, K, split))
+    b.quantize_act_grouped(to_dev_bf16(xb), g, _perm_arg(perms), split, out=a)
+    wide = torch.full((tokens + 2, 88), 7.0, dtype=torch.bfloat16, device="cuda")
+    b.gemm_grouped(a, w, g, y=wide[1:-1, 8:78])
+    torch.cuda.synchronize()
+    assert bool((wide[0] == 7).all() and (wide[-1] == 7).all() and (wide[:, :8] == 7).all() and (wide[:, 78:] == 7).all())
+    assert torch.equal(w.q4, before) and bool((g.map == word).all())
+
+
 # ---- matrix-vector products ----
 
 
