@@ -405,15 +405,22 @@ mm::ExpertStride expert_stride(const mm_mx_tensor* w) {
   return mm::ExpertStride{{l.bytes[0], l.bytes[1], l.bytes[2]}, l.bytes[3]};
 }
 
-mm::GemmRoute route_grouped(const mm::GemmGroupedArgs& g, const mm::Device& dev) {
+mm::GroupedKernel route_grouped(const mm::GemmGroupedArgs& g, const mm::Device& dev) {
   mm::GroupedSizes sizes = {g.rows, g.experts, g.g.w.rows, {g.g.steps[0], g.g.steps[1], g.g.steps[2]}, dev.cus, {}};
   for (int k = 0; k < mm::kTileLists; ++k) sizes.ntiles[k] = g.ntiles[k];
   return mm::grouped_route(sizes);
 }
 
-hipError_t launch_gemm_grouped(const mm::GemmGroupedArgs& g, const mm::GemmRoute& r, const mm::Device& dev, hipStream_t s) {
-  if (r.kernel == mm::GemmKernel::kSplit) return mm::launch_gemm_split_grouped(g, r.shape, dev, s);
-  return mm::launch_gemm_tiled_grouped(g, r.kernel == mm::GemmKernel::kTiled256, dev, s);
+hipError_t launch_gemm_grouped(const mm::GemmGroupedArgs& g, mm::GroupedKernel k, const mm::Device& dev, hipStream_t s) {
+  switch (k) {
+    case mm::GroupedKernel::kSplit32x32: return mm::launch_gemm_split_grouped(g, false, dev, s);
+    case mm::GroupedKernel::kSplit64x32: return mm::launch_gemm_split_grouped(g, true, dev, s);
+    case mm::GroupedKernel::kTiled128x128: return mm::launch_gemm_tiled_grouped(g, 128, 128, dev, s);
+    case mm::GroupedKernel::kTiled256x128: return mm::launch_gemm_tiled_grouped(g, 256, 128, dev, s);
+    case mm::GroupedKernel::kTiled256x256: return mm::launch_gemm_tiled_grouped(g, 256, 256, dev, s);
+    case mm::GroupedKernel::kNone: break;
+  }
+  return hipErrorInvalidValue;
 }
 
 }  // namespace
@@ -540,9 +547,9 @@ mm_status mm_gemm_grouped(const mm_mx_tensor* a, const mm_mx_tensor* w, const mm
   mm::Device dev;
   hipError_t e = mm::current_device(&dev);
   if (e == hipSuccess) {
-    const mm::GemmRoute r = route_grouped(g, dev);
-    if (r.shape < 0) return fail(MM_ERR_SHAPE, "%s: more tiles than a launch takes", who);
-    e = launch_gemm_grouped(g, r, dev, static_cast<hipStream_t>(stream));
+    const mm::GroupedKernel k = route_grouped(g, dev);
+    if (k == mm::GroupedKernel::kNone) return fail(MM_ERR_SHAPE, "%s: more tiles than a launch takes", who);
+    e = launch_gemm_grouped(g, k, dev, static_cast<hipStream_t>(stream));
   }
   if (e != hipSuccess) return fail(MM_ERR_DEVICE, "%s: launch failed: %s", who, hipGetErrorString(e));
   return MM_OK;

@@ -147,9 +147,9 @@ struct AllRows {
   __device__ __forceinline__ int row(int, int lane) const { return lane & 31; }
 };
 struct FirstRows {
-  int n;  // at least 1
-  __device__ __forceinline__ int fragment(int j) const { return j == 0 || 32 * j < n ? j : 0; }
-  __device__ __forceinline__ int row(int j, int lane) const { return 32 * j + (lane & 31) < n ? lane & 31 : 0; }
+  int n;  // at least 1, of one fragment
+  __device__ __forceinline__ int fragment(int j) const { return j; }
+  __device__ __forceinline__ int row(int, int lane) const { return (lane & 31) < n ? lane & 31 : 0; }
 };
 
 template <int G, int TN, int TM, class Rows>
@@ -402,18 +402,18 @@ __global__ __launch_bounds__(kThreads) void gemm_split_kernel(GemmArgs a, int ti
   tile_product<TN, TM, FS>(a, lds, n0, n_own, m0, w0, w1, w2, AllRows{}, RowsInPlace{m_own, a.x.rows});
 }
 
-// tiles_m: the length of the tile list, known to the host; how many of its tiles
-// there are only the device knows, the others' workgroups end at once.
-template <int TN, int TM, int FS>
-__global__ __launch_bounds__(kThreads) void gemm_split_grouped_kernel(GemmGroupedArgs a, const RowTile* tiles, int tiles_n,
-                                                                      int tiles_m, int w0, int w1, int w2) {
+// The grouped form: 32 TN weight rows by a row group.  tiles_m: the length of the tile
+// list, known to the host; how many of its tiles there are only the device knows, the
+// others' workgroups end at once.
+template <int TN, int FS>
+__global__ __launch_bounds__(kThreads) void gemm_split_grouped_kernel(GemmGroupedArgs a, int tiles_n, int tiles_m, int w0, int w1,
+                                                                      int w2) {
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
   const int id = tile_of(tiles_n * tiles_m);
   const int tn = id / tiles_m, tm = id - tn * tiles_m;
-  const RowTile t = tiles[tm];
-  const TileRows r = tile_rows(t, 32 * TM, a.g.x.rp, a.experts);
-  const int n = r.rows;
-  if (n == 0) return;  // uniform
+  const RowTile t = a.tiles[0][tm];
+  const TileRows r = tile_rows(t, kRowGroup, a.g.x.rp, a.experts);
+  if (r.rows == 0) return;  // uniform
   const int64_t e = r.expert;
   GemmArgs g = a.g;
 #pragma unroll
@@ -421,7 +421,7 @@ __global__ __launch_bounds__(kThreads) void gemm_split_grouped_kernel(GemmGroupe
   g.w.sc += e * a.next.sc;
   const int64_t n_own = (int64_t)tn * (32 * TN), m0 = (int64_t)t.first * kRowGroup;
   const int64_t n0 = n_own + 32 * TN <= g.w.rp ? n_own : g.w.rp - 32 * TN;
-  tile_product<TN, TM, FS>(g, lds, n0, n_own, m0, w0, w1, w2, FirstRows{n}, RowsBySlot{a.slots, m0 + n, a.rows});
+  tile_product<TN, 1, FS>(g, lds, n0, n_own, m0, w0, w1, w2, FirstRows{r.rows}, RowsBySlot{a.slots, m0 + r.rows, a.rows});
 }
 
 template <int TN, int TM, int FS>
@@ -468,41 +468,34 @@ hipError_t launch_gemm_split(const GemmArgs& a, int shape, const Device& dev, hi
 
 // ---- the grouped form ----
 
-template <int I, int FS>
+template <int TN, int FS>
 static hipError_t launch_grouped_fs(const GemmGroupedArgs& a, const Device& dev, hipStream_t stream) {
-  constexpr int TN = kSplitShapes[I].tn, TM = kSplitShapes[I].tm;
-  constexpr int kList = TM == 1 ? 0 : 1;
-  static_assert(32 * TM == kTileRows[kList], "a listed tile size");
-  constexpr int lds = lds_bytes<TN, TM>();
+  static_assert(kTileRows[0] == kRowGroup, "the first list's tiles are row groups");
+  constexpr int lds = lds_bytes<TN, 1>();
   static DeviceOnce once;
-  hipError_t e = allow_lds(once, dev, reinterpret_cast<const void*>(gemm_split_grouped_kernel<TN, TM, FS>), lds);
+  hipError_t e = allow_lds(once, dev, reinterpret_cast<const void*>(gemm_split_grouped_kernel<TN, FS>), lds);
   if (e != hipSuccess) return e;
-  const int64_t tn = (a.g.w.rows + 32 * TN - 1) / (32 * TN), tm = a.ntiles[kList];
+  const int64_t tn = (a.g.w.rows + 32 * TN - 1) / (32 * TN), tm = a.ntiles[0];
   int w[3];
   share_waves(a.g.steps, kByteCost, kWaves, w);
-  hipLaunchKernelGGL((gemm_split_grouped_kernel<TN, TM, FS>), dim3((unsigned)(tn * tm)), dim3(kThreads), lds, stream, a,
-                     a.tiles[kList], (int)tn, (int)tm, w[0], w[1], w[2]);
+  hipLaunchKernelGGL((gemm_split_grouped_kernel<TN, FS>), dim3((unsigned)(tn * tm)), dim3(kThreads), lds, stream, a, (int)tn,
+                     (int)tm, w[0], w[1], w[2]);
   return hipGetLastError();
 }
 
-template <int I>
-static hipError_t launch_shape_grouped(const GemmGroupedArgs& a, const Device& dev, hipStream_t stream) {
+template <int TN>
+static hipError_t launch_grouped(const GemmGroupedArgs& a, const Device& dev, hipStream_t stream) {
   switch (a.g.fs) {
-    case 0: return launch_grouped_fs<I, 0>(a, dev, stream);
-    case 1: return launch_grouped_fs<I, 1>(a, dev, stream);
-    case 2: return launch_grouped_fs<I, 2>(a, dev, stream);
-    case 3: return launch_grouped_fs<I, 3>(a, dev, stream);
+    case 0: return launch_grouped_fs<TN, 0>(a, dev, stream);
+    case 1: return launch_grouped_fs<TN, 1>(a, dev, stream);
+    case 2: return launch_grouped_fs<TN, 2>(a, dev, stream);
+    case 3: return launch_grouped_fs<TN, 3>(a, dev, stream);
   }
   return hipErrorInvalidValue;
 }
 
-hipError_t launch_gemm_split_grouped(const GemmGroupedArgs& a, int shape, const Device& dev, hipStream_t stream) {
-  switch (shape) {
-    case 0: return launch_shape_grouped<0>(a, dev, stream);
-    case 1: return launch_shape_grouped<1>(a, dev, stream);
-    case 4: return launch_shape_grouped<4>(a, dev, stream);
-  }
-  return hipErrorInvalidValue;
+hipError_t launch_gemm_split_grouped(const GemmGroupedArgs& a, bool wide, const Device& dev, hipStream_t stream) {
+  return wide ? launch_grouped<2>(a, dev, stream) : launch_grouped<1>(a, dev, stream);
 }
 
 }  // namespace mm

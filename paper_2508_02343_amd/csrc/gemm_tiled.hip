@@ -48,6 +48,17 @@
 // XCD by XCD and in groups of weight tiles, so the tiles that run together
 // on one XCD share its L2.
 //
+// Products grouped by expert (mm_gemm_grouped) run the same kernel over a list of
+// their experts' tiles (Grouped below), with a third tile shape, 128 x 128, of which a
+// CU holds two workgroups: for products of a few rounds of tiles, where one tile's
+// set-up, first loads and drain (4-5 of 16 us at K 2080, 256 x 128) otherwise leave
+// the CU idle.  Measured (us, GEMM alone, 256 x 128 / 256 x 256 / 128 x 128): 4096 slots x
+// 4096 x 14336 on 8 experts 200 / 193 / 210, 8192 x 14336 x 4096 323 / 303 / 342, 3108
+// ragged slots x 2080 x 5400 on 16 54 / 53 / 60, 3000 x 8192 x 1024 on 4 33 / 50 / 27, 512 x
+// 4096 x 4096 on 2 19.7 / 31 / 17.  What bounds the K loop is shared by all three: a
+// stage takes about twice its MFMAs' time, as the operands' LDS reads and the LDS
+// writes of the loads together take as long as the MFMAs.
+//
 // Measured (us, M x K x N): without the producers and with the waits between
 // the stages 2048 x 4096 x 4096 took 29.9 (with them 27.0), 1000 x 4096 x 5400 in
 // E2M3 / E5M2 30.1 (26.6), 700 x 4096 x 14336 44.0 (39.4); the 256 x 256 tile
@@ -90,15 +101,19 @@ struct Tile {
   // against 512 of its MFMAs, and a wavefront that issues both in order has its
   // MFMAs wait behind its loads (stage times on 2048 x 4096 x 4096: MFMAs
   // alone 275 ns, with the LDS reads 410, with the loads 390, with both 540).
-  static constexpr bool kProducers = BM == 128;
+  static constexpr bool kProducers = BN == 256 && BM == 128;
   static constexpr int kThreads = 64 * kWaves * (kProducers ? 2 : 1);
   static constexpr int kSlots = kProducers ? 6 : 4;
   // a wavefront's loads of a stage: a quarter of each operand's codes, and a
   // scale load
   static constexpr int kLoadsW = BN / 64, kLoadsX = BM / 64;
   static constexpr int kCodeLoads = kLoadsW + kLoadsX, kLoads = kCodeLoads + 1;
-  static_assert(BN == 256 && (BM == 256 || BM == 128), "tile shapes");
-  static_assert(kSlots * kSlotBytes <= kLdsBytes, "the ring fits LDS");
+  // 128 x 128 (grouped products): two workgroups to a CU, each with one wavefront
+  // per SIMD, so that one's set-up, first loads and drain run behind the other's MFMAs
+  static constexpr int kPerCu = BN == 128 ? 2 : 1;
+  static constexpr int kLds = kLdsBytes / kPerCu;
+  static_assert((BN == 256 && (BM == 256 || BM == 128)) || (BN == 128 && BM == 128), "tile shapes");
+  static_assert(kSlots * kSlotBytes <= kLds, "the ring fits LDS");
   static_assert((kSlots - 1) * kLoads < 64, "vmcnt range");
 };
 
@@ -472,7 +487,8 @@ __device__ __forceinline__ void mfma_block(const Ctx<BN, BM>& c, Acc<BN, BM>& ac
   constexpr int TN = Ti::TN, TM = Ti::TM, F = Ti::F, NS = Ti::kSlots;
   constexpr int kPer = TN * TM;
   constexpr int kM = stage_slices(G) * kPer;
-  constexpr int kR = kM == 8 ? 4 : kM * 3 / 4, kS = kM - 3;
+  constexpr int kR = kM == 4 ? 2 : (kM == 8 ? 4 : kM * 3 / 4), kS = kR + 1;
+  constexpr int kSh = kM == 4 ? 3 : kM - 2;  // the first half of the scale shifts: behind the wait
   if constexpr (T < kM) {
     constexpr int fmt = group_fmt(G, FS);
     constexpr int KK = T / kPer, i = (T % kPer) / TM, j = T % TM;
@@ -496,7 +512,7 @@ __device__ __forceinline__ void mfma_block(const Ctx<BN, BM>& c, Acc<BN, BM>& ac
       if constexpr (!Ti::kProducers) wait_vmcnt<(NS - 2) * Ti::kLoads>();
       barrier();
     }
-    if constexpr (T == kM - 2) shift_scales<0, F / 2>(nxt, l.shift);
+    if constexpr (T == kSh) shift_scales<0, F / 2>(nxt, l.shift);
     if constexpr (T == kM - 1) {
       shift_scales<F / 2, F>(nxt, l.shift);
       if constexpr (G >= 1) l.shift ^= 16;
@@ -655,7 +671,7 @@ struct Grouped {
 // workgroups past those that there are end at once, so that the tiles go evenly to
 // the XCDs).
 template <int BN, int BM, int FS, class Args>
-__global__ __launch_bounds__((Tile<BN, BM>::kThreads), 1) void gemm_tiled_kernel(Args args) {
+__global__ __launch_bounds__((Tile<BN, BM>::kThreads), (Tile<BN, BM>::kPerCu)) void gemm_tiled_kernel(Args args) {
   using T = Tile<BN, BM>;
   constexpr bool kGrouped = std::is_same_v<Args, Grouped>;
   GemmArgs a;
@@ -780,12 +796,12 @@ __global__ __launch_bounds__((Tile<BN, BM>::kThreads), 1) void gemm_tiled_kernel
   wait_lgkm0();
   barrier();
   constexpr int kRowStride = BN * 2 + 16;
-  static_assert(BM * kRowStride <= kLdsBytes, "epilogue tile fits LDS");
+  static_assert(BM * kRowStride <= T::kLds, "epilogue tile fits LDS");
   const int r = c.lane & 31, g = c.lane >> 5;
   // grouped: the rows' slots, behind the tile in LDS (-1: none); loaded while the
   // accumulators are rounded, as a load in front of every store would hold it back
   constexpr int kSlotsOff = BM * kRowStride;
-  static_assert(kSlotsOff + BM * 4 <= kLdsBytes && BM <= T::kThreads, "a slot per row");
+  static_assert(kSlotsOff + BM * 4 <= T::kLds && BM <= T::kThreads, "a slot per row");
   int32_t slot = -1;
   if constexpr (kGrouped)
     if ((int)threadIdx.x < filled) slot = args.g.slots[m0 + threadIdx.x];
@@ -813,13 +829,7 @@ __global__ __launch_bounds__((Tile<BN, BM>::kThreads), 1) void gemm_tiled_kernel
   __syncthreads();
   constexpr int kChunks = BN / 8;  // 16-byte chunks per row
   const int64_t M = a.x.rows, N = a.w.rows;
-  for (int ch = threadIdx.x; ch < BM * kChunks; ch += T::kThreads) {
-    const int rr = ch / kChunks, col = (ch - rr * kChunks) * 8;
-    int64_t m = m0 + rr;
-    const int64_t n = n0 + col;
-    if constexpr (kGrouped) m = lds_read<int32_t>(c.lds0 + kSlotsOff + 4 * rr);
-    if ((kGrouped ? m < 0 : m >= M) || n >= N) continue;
-    const u32x4 v = lds_read<u32x4>(c.lds0 + rr * kRowStride + col * 2);
+  auto store = [&](int64_t m, int64_t n, const u32x4& v) {
     uint16_t* dst = a.y + m * a.ldy + n;
     if (n + 8 <= N) {
       // streamed: the output is not read again here, and keeping it out of
@@ -831,16 +841,46 @@ __global__ __launch_bounds__((Tile<BN, BM>::kThreads), 1) void gemm_tiled_kernel
         dst[e] = (uint16_t)(wd >> (16 * (e & 1)));
       }
     }
+  };
+  if constexpr (kGrouped) {
+    // four rows' slots and words at a time (one after the other, each store waited for
+    // two LDS reads: 4.0 us of a 256 x 256 tile's 38)
+    constexpr int kStep = T::kThreads / kChunks, kTurns = BM / kStep, kU = 4;
+    static_assert(T::kThreads % kChunks == 0 && BM % kStep == 0 && kTurns % kU == 0, "whole turns");
+    const int col = (int)threadIdx.x % kChunks * 8, row0 = (int)threadIdx.x / kChunks;
+    const int64_t n = n0 + col;
+    if (n >= N) return;
+    for (int k0 = 0; k0 < kTurns; k0 += kU) {
+      if (row0 + k0 * kStep >= filled) break;  // (this row and those behind it have none)
+      int32_t to[kU];
+      u32x4 v[kU];
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const int rr = row0 + (k0 + u) * kStep;
+        to[u] = lds_read<int32_t>(c.lds0 + kSlotsOff + 4 * rr);
+        v[u] = lds_read<u32x4>(c.lds0 + rr * kRowStride + col * 2);
+      }
+#pragma unroll
+      for (int u = 0; u < kU; ++u)
+        if (to[u] >= 0) store(to[u], n, v[u]);
+    }
+  } else {
+    for (int ch = threadIdx.x; ch < BM * kChunks; ch += T::kThreads) {
+      const int rr = ch / kChunks, col = (ch - rr * kChunks) * 8;
+      const int64_t m = m0 + rr, n = n0 + col;
+      if (m >= M || n >= N) continue;
+      store(m, n, lds_read<u32x4>(c.lds0 + rr * kRowStride + col * 2));
+    }
   }
 }
 
 template <int BN, int BM, int FS, class Args>
 static hipError_t launch_tile_fs(const Args& a, int64_t tiles, const Device& dev, hipStream_t stream) {
   static DeviceOnce once;
-  hipError_t e = allow_lds(once, dev, reinterpret_cast<const void*>(gemm_tiled_kernel<BN, BM, FS, Args>), kLdsBytes);
+  hipError_t e = allow_lds(once, dev, reinterpret_cast<const void*>(gemm_tiled_kernel<BN, BM, FS, Args>), Tile<BN, BM>::kLds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((gemm_tiled_kernel<BN, BM, FS, Args>), dim3((unsigned)tiles), dim3(Tile<BN, BM>::kThreads), kLdsBytes,
-                     stream, a);
+  hipLaunchKernelGGL((gemm_tiled_kernel<BN, BM, FS, Args>), dim3((unsigned)tiles), dim3((Tile<BN, BM>::kThreads)),
+                     (Tile<BN, BM>::kLds), stream, a);
   return hipGetLastError();
 }
 
@@ -874,8 +914,9 @@ hipError_t launch_gemm_tiled(const GemmArgs& a, bool square, const Device& dev, 
   return square ? launch_plain<256, 256>(a, dev, stream) : launch_plain<256, 128>(a, dev, stream);
 }
 
-hipError_t launch_gemm_tiled_grouped(const GemmGroupedArgs& a, bool square, const Device& dev, hipStream_t stream) {
-  return square ? launch_grouped<256, 256>(a, dev, stream) : launch_grouped<256, 128>(a, dev, stream);
+hipError_t launch_gemm_tiled_grouped(const GemmGroupedArgs& a, int bn, int bm, const Device& dev, hipStream_t stream) {
+  if (bn == 128) return launch_grouped<128, 128>(a, dev, stream);
+  return bm == 128 ? launch_grouped<256, 128>(a, dev, stream) : launch_grouped<256, 256>(a, dev, stream);
 }
 
 }  // namespace mm

@@ -119,9 +119,10 @@ struct GemmGroupedArgs {
   int64_t rows;  // slots
   int experts;
 };
-hipError_t launch_gemm_tiled_grouped(const GemmGroupedArgs& a, bool square, const Device& dev, hipStream_t stream);
-// shape: 0, 1 or 4 of kSplitShapes
-hipError_t launch_gemm_split_grouped(const GemmGroupedArgs& a, int shape, const Device& dev, hipStream_t stream);
+// tiles of bn weight rows by bm rows: 128 x 128, 256 x 128, 256 x 256
+hipError_t launch_gemm_tiled_grouped(const GemmGroupedArgs& a, int bn, int bm, const Device& dev, hipStream_t stream);
+// 64 x 32 (weights of at least 64 padded rows), else 32 x 32
+hipError_t launch_gemm_split_grouped(const GemmGroupedArgs& a, bool wide, const Device& dev, hipStream_t stream);
 
 // At most this many rows in a call of the matrix-vector kernel.
 constexpr int kGemvMaxRows = 16;

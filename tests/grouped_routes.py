@@ -21,19 +21,16 @@ int main() {
                &z.steps[2], &z.cus, v + 3, v + 4, v + 5) == 10) {
     z.slots = v[0], z.experts = v[1], z.n = v[2];
     for (int k = 0; k < 3; ++k) z.ntiles[k] = v[3 + k];
-    const mm::GemmRoute r = mm::grouped_route(z);
-    int tn = 8, tm = r.kernel == mm::GemmKernel::kTiled256 ? 8 : 4, list = tm == 8 ? 2 : 1;
-    if (r.shape < 0) {
-      puts("none 0 0");
-      continue;
-    }
-    if (r.kernel == mm::GemmKernel::kSplit) {
-      tn = mm::kSplitShapes[r.shape].tn;
-      tm = mm::kSplitShapes[r.shape].tm;
-      list = tm == 1 ? 0 : 1;
-    }
-    printf("%%s%%dx%%d %%lld %%d\\n", r.kernel == mm::GemmKernel::kSplit ? "split" : "tiled", 32 * tn, 32 * tm,
-           (long long)(mm::ceil_div(z.n, 32 * tn) * z.ntiles[list]), tm == 8 ? 256 : 512);
+    const mm::GroupedKernel k = mm::grouped_route(z);
+    const char* kind = k <= mm::GroupedKernel::kSplit64x32 ? "split" : "tiled";
+    bool found = false;
+    for (const mm::GroupedChoice& c : mm::kGroupedChoices)
+      if (c.kernel == k) {
+        found = true;
+        printf("%%s%%dx%%d %%lld %%d\\n", kind, 32 * c.tn, 32 * c.tm, (long long)(mm::ceil_div(z.n, 32 * c.tn) * z.ntiles[c.list]),
+               c.threads);
+      }
+    if (!found) puts("none 0 0");
   }
 }
 """
@@ -63,7 +60,7 @@ def route(slots: int, experts: int, N: int, split, cus: int = 256) -> tuple[str,
 CASES = [  # kernel, slots, experts, N, split
     ("split32x32", 13, 4, 301, (160, 96, 64)),
     ("split64x32", 2900, 3, 150, (224, 64, 96)),
-    ("split64x128", 1500, 2, 1400, (1152, 288, 1280)),
-    ("tiled256x128", 4000, 3, 700, (128, 64, 160)),
-    ("tiled256x256", 4000, 2, 4415, (1920, 480, 2432)),
+    ("tiled128x128", 4000, 3, 700, (128, 64, 160)),
+    ("tiled256x128", 2980, 2, 2300, (160, 64, 192)),
+    ("tiled256x256", 4700, 2, 5400, (704, 160, 832)),
 ]
