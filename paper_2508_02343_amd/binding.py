@@ -7,6 +7,7 @@ is missing the import of this module fails loudly; there is no fallback.
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import functools
 import os
@@ -137,6 +138,7 @@ def _load_packed(path: str = LIB_PATH) -> ctypes.CDLL:
 _fast = _load_packed()
 
 _BF16, _INT32 = torch.bfloat16, torch.int32
+_CURRENT = contextlib.nullcontext()
 
 
 class MMError(RuntimeError):
@@ -415,6 +417,12 @@ class MXStack:
     _packed = MXTensor._packed  # the first expert's descriptor
 
 
+def _new_on(stream):
+    """Within it new tensors are the call's stream's: their zeros and the earlier use of
+    their memory come before the call's kernels, their reuse after them."""
+    return _CURRENT if stream is None else torch.cuda.stream(stream)
+
+
 def _here(index: int, name: str) -> None:
     """A tensor's device is the current one (kernels are launched there)."""
     if index < 0 or index != (torch.cuda.current_device() if _raw_device is None else _raw_device()):
@@ -492,7 +500,8 @@ def group_rows(ids: torch.Tensor, experts: int, out: RowGroups | None = None, st
     index = ids.get_device()
     _here(index, "ids")
     if out is None:
-        out = RowGroups.empty(ids.numel(), experts, device=ids.device)
+        with _new_on(stream):
+            out = RowGroups.empty(ids.numel(), experts, device=ids.device)
     elif out.rows != ids.numel() or out.experts != experts or out.device_index != index:
         raise ValueError(f"out is for {out.rows} slots of {out.experts} experts, got {ids.numel()} of {experts}")
     _check(_fast.mm_group_rows(ids.data_ptr(), out._packed(), _stream_int(stream)))
@@ -513,7 +522,8 @@ def quantize_act_grouped(x: torch.Tensor, groups: RowGroups, perm: torch.Tensor,
     if type(split) is not tuple:
         split = tuple(map(int, split))
     if out is None:
-        out = MXTensor.empty(groups.capacity, K, split, device=x.device, formats=formats)
+        with _new_on(stream):
+            out = MXTensor.empty(groups.capacity, K, split, device=x.device, formats=formats)
     elif out.rows != groups.capacity or out.K != K or tuple(out.split) != split:
         raise ValueError(f"out is [{out.rows}, {out.K}] split {tuple(out.split)}, expected [{groups.capacity}, {K}] split {split}")
     _check(_fast.mm_quantize_act_grouped(x.data_ptr(), x.stride(0), top_k, perm.data_ptr(), stride, groups._packed(),
@@ -521,10 +531,11 @@ def quantize_act_grouped(x: torch.Tensor, groups: RowGroups, perm: torch.Tensor,
     return out
 
 
-def _result(y: torch.Tensor | None, M: int, N: int, index: int, device) -> torch.Tensor:
+def _result(y: torch.Tensor | None, M: int, N: int, index: int, device, stream=None) -> torch.Tensor:
     """A bf16 [M, N] result; a new one is zero, as some of its rows may not be written."""
     if y is None:
-        return torch.zeros((M, _round16(N) if N % 8 else N), dtype=torch.bfloat16, device=device)[:, :N]
+        with _new_on(stream):
+            return torch.zeros((M, _round16(N) if N % 8 else N), dtype=torch.bfloat16, device=device)[:, :N]
     if y.dtype is not _BF16 or y.shape != (M, N) or y.stride(1) != 1 or y.get_device() != index:
         raise ValueError(f"y must be a bfloat16 [{M}, {N}] tensor with unit column stride on {device}")
     return y
@@ -541,7 +552,7 @@ def gemm_grouped(a: MXTensor, w: MXStack, groups: RowGroups, y: torch.Tensor | N
         raise ValueError(f"a has {a.rows} rows, the groups' capacity is {groups.capacity}")
     if not isinstance(w, MXStack) or w.count != groups.experts:
         raise ValueError(f"w must be an MXStack of the groups' {groups.experts} experts")
-    y = _result(y, groups.rows, w.rows, index, groups.map.device)
+    y = _result(y, groups.rows, w.rows, index, groups.map.device, stream)
     _check(_fast.mm_gemm_grouped(_packed_checked(a, index, "a"), _packed_checked(w, index, "w", w.count),
                                  groups._packed(), y.data_ptr(), y.stride(0), _stream_int(stream)))
     return y
@@ -590,9 +601,10 @@ def gemv(x: torch.Tensor, w: MXTensor | MXStack, perm: torch.Tensor, ids: torch.
     else:
         n_ws = gemv_workspace_size(rows, K, w.split) if type(w.split) is not tuple else _gemv_workspace(rows, K, w.split)
         if n_ws:
-            workspace = torch.empty(n_ws, dtype=torch.uint8, device=x.device)
+            with _new_on(stream):
+                workspace = torch.empty(n_ws, dtype=torch.uint8, device=x.device)
             p_ws = workspace.data_ptr()
-    y = _result(y, rows, w.rows, index, x.device)
+    y = _result(y, rows, w.rows, index, x.device, stream)
     _check(_fast.mm_gemv(x.data_ptr(), x.stride(0), rows, top_k, perm.data_ptr(), stride,
                          _packed_checked(w, index, "w", experts), experts, p_ids, p_ws, n_ws, y.data_ptr(), y.stride(0),
                          _stream_int(stream)))

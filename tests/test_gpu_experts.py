@@ -452,3 +452,34 @@ def test_two_streams():
     torch.cuda.synchronize()
     for i in (0, 1):
         assert torch.equal(got[i][0], want[i][0]) and torch.equal(got[i][1], want[i][1]), i
+
+
+def test_new_tensors_belong_to_the_call_stream():
+    """stream=: what a call allocates is ordered with its kernels, not with the current stream, which is busy here."""
+    note("stream= and new tensors")
+    b = _b()
+    T, k, E, N, split = 5, 2, 4, 520, (12288, 3584, 512)  # (gemv of ten rows: with a workspace)
+    K = sum(split)
+    xb, perms = C.activations(T, K, 1, seed=61)
+    w = _stack(C.weights(E, N, K, seed=62), perms, split)
+    perm, x = _perm_arg(perms), to_dev_bf16(xb)
+    ids = _dev_ids(C.make_ids(T * k, E, "even", seed=9))
+    assert b.gemv_workspace_size(T * k, K, split) > 0
+
+    def layer(stream):
+        g = b.group_rows(ids, E, stream=stream)
+        q = b.quantize_act_grouped(x, g, perm, split, top_k=k, stream=stream)
+        return b.gemm_grouped(q, w, g, stream=stream), b.gemv(x, w, perm, ids=ids, top_k=k, stream=stream)
+
+    want = [t.clone() for t in layer(None)]
+    other, busy = torch.cuda.Stream(), torch.zeros(1 << 28, device="cuda")
+    torch.cuda.synchronize()
+    for turn in range(3):
+        for _ in range(100):
+            busy.add_(1.0)
+        got = layer(other)
+        scratch = [torch.full((1 << 20,), 7, dtype=torch.uint8, device="cuda") for _ in range(8)]  # (behind the freed workspace)
+        torch.cuda.synchronize()
+        for a, e in zip(got, want):
+            assert torch.equal(a, e), turn
+        del scratch
