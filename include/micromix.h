@@ -369,7 +369,7 @@ mm_status mm_quantize_act_grouped(const void* x_bf16, int64_t ldx, int64_t top_k
  *           the other, every mm_mx_layout_sizes() bytes.
  *   y_bf16  device, bf16 [groups->rows, N] row-major, row stride ldy elements
  *           (ldy >= N, ldy % 8 == 0, 16-byte aligned).
- * The launch depends on the sizes only, so it can be captured and replayed with
+ * The launches depend on the sizes only, so they can be captured and replayed with
  * other ids.  Errors: those of mm_gemm.
  */
 mm_status mm_gemm_grouped(const mm_mx_tensor* a, const mm_mx_tensor* w, const mm_row_groups* groups, void* y_bf16,

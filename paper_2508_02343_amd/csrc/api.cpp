@@ -415,9 +415,10 @@ hipError_t launch_gemm_grouped(const mm::GemmGroupedArgs& g, mm::GroupedKernel k
   switch (k) {
     case mm::GroupedKernel::kSplit32x32: return mm::launch_gemm_split_grouped(g, false, dev, s);
     case mm::GroupedKernel::kSplit64x32: return mm::launch_gemm_split_grouped(g, true, dev, s);
-    case mm::GroupedKernel::kTiled128x128: return mm::launch_gemm_tiled_grouped(g, 128, 128, dev, s);
-    case mm::GroupedKernel::kTiled256x128: return mm::launch_gemm_tiled_grouped(g, 256, 128, dev, s);
-    case mm::GroupedKernel::kTiled256x256: return mm::launch_gemm_tiled_grouped(g, 256, 256, dev, s);
+    case mm::GroupedKernel::kTiled128x128: return mm::launch_gemm_tiled_grouped(g, 128, 128, false, dev, s);
+    case mm::GroupedKernel::kTiled256x128: return mm::launch_gemm_tiled_grouped(g, 256, 128, false, dev, s);
+    case mm::GroupedKernel::kTiled256x256: return mm::launch_gemm_tiled_grouped(g, 256, 256, false, dev, s);
+    case mm::GroupedKernel::kTiled256x256Rest: return mm::launch_gemm_tiled_grouped(g, 256, 256, true, dev, s);
     case mm::GroupedKernel::kNone: break;
   }
   return hipErrorInvalidValue;

@@ -665,25 +665,48 @@ struct Grouped {
   const RowTile* tiles;
   int tiles_m;           // activation tiles that there may be
   const int32_t* count;  // and that there are: only the device knows
+  int whole;             // 0, or the CUs: the Rest takes a last round that is at most half full
 };
+// The 256 x 256 tiles of such a last round, in quarters of 128 x 128: two to a CU, they take
+// about half of the round's time (us, 8192 rows of two of eight experts, K 14336 x N 4096,
+// 2.25 rounds, 301 -> 274; 4096 rows, 4096 x 14336, 4.4 rounds, 187 -> 183; where nothing
+// is left to them the launch costs 1.5-2).
+struct Rest {
+  Grouped of;
+};
+// How many of nt tiles are not the Rest's.
+__device__ __forceinline__ int in_rounds(int nt, int whole) {
+  const int rest = whole ? nt % whole : 0;
+  return 2 * rest <= whole ? nt - rest : nt;
+}
 
-// Args: Plain or Grouped (the grid covers as many tiles as there may be; the
+// Args: Plain, Grouped or Rest (the grid covers as many tiles as there may be; the
 // workgroups past those that there are end at once, so that the tiles go evenly to
 // the XCDs).
 template <int BN, int BM, int FS, class Args>
 __global__ __launch_bounds__((Tile<BN, BM>::kThreads), (Tile<BN, BM>::kPerCu)) void gemm_tiled_kernel(Args args) {
   using T = Tile<BN, BM>;
-  constexpr bool kGrouped = std::is_same_v<Args, Grouped>;
+  constexpr bool kRest = std::is_same_v<Args, Rest>, kGrouped = kRest || std::is_same_v<Args, Grouped>;
   GemmArgs a;
-  const int tiles_n = args.tiles_n;
-  int tiles_m;
+  const auto& shape = [&]() -> const auto& {
+    if constexpr (kRest) return args.of;
+    else return args;
+  }();
+  const int tiles_n = shape.tiles_n;
+  int tiles_m, nt, t_first = 0;
   if constexpr (kGrouped) {
-    tiles_m = *args.count;
-    tiles_m = tiles_m < args.tiles_m ? tiles_m : args.tiles_m;
-    if ((int)blockIdx.x >= tiles_n * tiles_m) return;  // uniform
-    a = args.g.g;
+    tiles_m = *shape.count;
+    tiles_m = tiles_m < shape.tiles_m ? tiles_m : shape.tiles_m;
+    nt = in_rounds(tiles_n * tiles_m, shape.whole);
+    if constexpr (kRest) {
+      t_first = nt;
+      nt = 4 * (tiles_n * tiles_m - nt);
+    }
+    if ((int)blockIdx.x >= nt) return;  // uniform
+    a = shape.g.g;
   } else {
     tiles_m = args.tiles_m;
+    nt = tiles_n * tiles_m;
     a = args.g;
   }
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
@@ -692,30 +715,32 @@ __global__ __launch_bounds__((Tile<BN, BM>::kThreads), (Tile<BN, BM>::kPerCu)) v
   // workgroup -> tile: consecutive tiles per XCD (workgroups are dealt to the
   // 8 XCDs round-robin), then groups of kGroupN weight tiles, activation
   // tiles fastest inside a group
-  const int nt = tiles_n * tiles_m;
   const int wg = blockIdx.x;
   const int xcd = wg & 7, kq = wg >> 3;
   const int per_x = nt >> 3, extra = nt & 7;
-  const int t = xcd * per_x + (xcd < extra ? xcd : extra) + kq;
+  int t = xcd * per_x + (xcd < extra ? xcd : extra) + kq;
+  const int part = t & 3;  // kRest: quarter of a tile
+  if constexpr (kRest) t = t_first + (t >> 2);
   const int grp = t / (kGroupN * tiles_m);
   const int within = t - grp * kGroupN * tiles_m;
   const int gn = tiles_n - grp * kGroupN < kGroupN ? tiles_n - grp * kGroupN : kGroupN;
   const int tn = grp * kGroupN + within % gn;
   const int tm = within / gn;
-  const int64_t n0 = (int64_t)tn * BN;
+  const int64_t n0 = kRest ? (int64_t)tn * (2 * BN) + (part & 1) * BN : (int64_t)tn * BN;
   int64_t m0 = (int64_t)tm * BM;
   int64_t x_rows = a.x.rp;  // activation rows that may be read
   int filled = 0;           // grouped: rows of the tile that hold a slot
   if constexpr (kGrouped) {
-    const RowTile t = args.tiles[tm];
-    const TileRows r = tile_rows(t, BM, a.x.rp, args.g.experts);
-    filled = r.rows;
-    if (filled == 0) return;  // uniform
+    const RowTile t = shape.tiles[tm];
+    const TileRows r = tile_rows(t, kRest ? 2 * BM : BM, a.x.rp, shape.g.experts);
+    const int front = kRest ? (part >> 1) * BM : 0;  // rows of the tile in front of this quarter
+    filled = r.rows - front < BM ? r.rows - front : BM;
+    if (filled <= 0 || n0 >= a.w.rows) return;  // uniform
     const int64_t e = r.expert;
 #pragma unroll
-    for (int k = 0; k < 3; ++k) a.w.q[k] += e * args.g.next.q[k];
-    a.w.sc += e * args.g.next.sc;
-    m0 = (int64_t)t.first * kRowGroup;
+    for (int k = 0; k < 3; ++k) a.w.q[k] += e * shape.g.next.q[k];
+    a.w.sc += e * shape.g.next.sc;
+    m0 = (int64_t)t.first * kRowGroup + front;
     x_rows = m0 + (filled + kRowGroup - 1) / kRowGroup * kRowGroup;
   }
 
@@ -804,7 +829,7 @@ __global__ __launch_bounds__((Tile<BN, BM>::kThreads), (Tile<BN, BM>::kPerCu)) v
   static_assert(kSlotsOff + BM * 4 <= T::kLds && BM <= T::kThreads, "a slot per row");
   int32_t slot = -1;
   if constexpr (kGrouped)
-    if ((int)threadIdx.x < filled) slot = args.g.slots[m0 + threadIdx.x];
+    if ((int)threadIdx.x < filled) slot = shape.g.slots[m0 + threadIdx.x];
   if (!producer) {
 #pragma unroll
     for (int i = 0; i < T::TN; ++i)
@@ -825,7 +850,7 @@ __global__ __launch_bounds__((Tile<BN, BM>::kThreads), (Tile<BN, BM>::kPerCu)) v
   if constexpr (kGrouped)
     if ((int)threadIdx.x < BM)
       *reinterpret_cast<__attribute__((address_space(3))) int32_t*>((uintptr_t)(c.lds0 + kSlotsOff + 4 * threadIdx.x)) =
-          slot < args.g.rows ? slot : -1;
+          slot < shape.g.rows ? slot : -1;
   __syncthreads();
   constexpr int kChunks = BN / 8;  // 16-byte chunks per row
   const int64_t M = a.x.rows, N = a.w.rows;
@@ -903,20 +928,25 @@ static hipError_t launch_plain(const GemmArgs& g, const Device& dev, hipStream_t
 }
 
 template <int BN, int BM>
-static hipError_t launch_grouped(const GemmGroupedArgs& g, const Device& dev, hipStream_t stream) {
+static hipError_t launch_grouped(const GemmGroupedArgs& g, bool rest, const Device& dev, hipStream_t stream) {
   constexpr int kList = BM == 128 ? 1 : 2;
   static_assert(BM == kTileRows[kList], "a listed tile size");
-  const Grouped a = {g, (int)((g.g.w.rows + BN - 1) / BN), g.tiles[kList], g.ntiles[kList], g.counts + kList};
-  return launch_tile<BN, BM>(a, g.g.fs, (int64_t)a.tiles_n * g.ntiles[kList], dev, stream);
+  const Grouped a = {g,           (int)((g.g.w.rows + BN - 1) / BN), g.tiles[kList], g.ntiles[kList], g.counts + kList,
+                     rest ? dev.cus : 0};
+  hipError_t e = launch_tile<BN, BM>(a, g.g.fs, (int64_t)a.tiles_n * g.ntiles[kList], dev, stream);
+  if (e != hipSuccess || !rest) return e;
+  // four quarters of at most half as many tiles as CUs
+  return launch_tile<128, 128>(Rest{a}, g.g.fs, 2 * (int64_t)a.whole, dev, stream);
 }
 
 hipError_t launch_gemm_tiled(const GemmArgs& a, bool square, const Device& dev, hipStream_t stream) {
   return square ? launch_plain<256, 256>(a, dev, stream) : launch_plain<256, 128>(a, dev, stream);
 }
 
-hipError_t launch_gemm_tiled_grouped(const GemmGroupedArgs& a, int bn, int bm, const Device& dev, hipStream_t stream) {
-  if (bn == 128) return launch_grouped<128, 128>(a, dev, stream);
-  return bm == 128 ? launch_grouped<256, 128>(a, dev, stream) : launch_grouped<256, 256>(a, dev, stream);
+hipError_t launch_gemm_tiled_grouped(const GemmGroupedArgs& a, int bn, int bm, bool rest, const Device& dev,
+                                     hipStream_t stream) {
+  if (bn == 128) return launch_grouped<128, 128>(a, false, dev, stream);
+  return bm == 128 ? launch_grouped<256, 128>(a, false, dev, stream) : launch_grouped<256, 256>(a, rest, dev, stream);
 }
 
 }  // namespace mm

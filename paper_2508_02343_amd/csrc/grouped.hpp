@@ -119,8 +119,10 @@ struct GemmGroupedArgs {
   int64_t rows;  // slots
   int experts;
 };
-// tiles of bn weight rows by bm rows: 128 x 128, 256 x 128, 256 x 256
-hipError_t launch_gemm_tiled_grouped(const GemmGroupedArgs& a, int bn, int bm, const Device& dev, hipStream_t stream);
+// tiles of bn weight rows by bm rows: 128 x 128, 256 x 128, 256 x 256 (rest: a last round that
+// is at most half full in quarters, by a launch of its own)
+hipError_t launch_gemm_tiled_grouped(const GemmGroupedArgs& a, int bn, int bm, bool rest, const Device& dev,
+                                     hipStream_t stream);
 // 64 x 32 (weights of at least 64 padded rows), else 32 x 32
 hipError_t launch_gemm_split_grouped(const GemmGroupedArgs& a, bool wide, const Device& dev, hipStream_t stream);
 

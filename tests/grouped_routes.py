@@ -27,7 +27,8 @@ int main() {
     for (const mm::GroupedChoice& c : mm::kGroupedChoices)
       if (c.kernel == k) {
         found = true;
-        printf("%%s%%dx%%d %%lld %%d\\n", kind, 32 * c.tn, 32 * c.tm, (long long)(mm::ceil_div(z.n, 32 * c.tn) * z.ntiles[c.list]),
+        printf("%%s%%dx%%d%%s %%lld %%d\\n", kind, 32 * c.tn, 32 * c.tm,
+               k == mm::GroupedKernel::kTiled256x256Rest ? "+rest" : "", (long long)(mm::ceil_div(z.n, 32 * c.tn) * z.ntiles[c.list]),
                c.threads);
       }
     if (!found) puts("none 0 0");
@@ -63,4 +64,5 @@ CASES = [  # kernel, slots, experts, N, split
     ("tiled128x128", 4000, 3, 700, (128, 64, 160)),
     ("tiled256x128", 2980, 2, 2300, (160, 64, 192)),
     ("tiled256x256", 4700, 2, 5400, (704, 160, 832)),
+    ("tiled256x256+rest", 3000, 2, 5400, (1024, 160, 832)),
 ]

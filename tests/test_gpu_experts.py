@@ -161,9 +161,10 @@ def test_quantize_grouped_widths(split, formats):
 
 
 def _grouped(tokens, top_k, experts, N, split, kind, formats=DEFAULT, own_sigma=False, seed=0, cols=None):
-    """The product's inputs on the GPU, and its reference (of the columns `cols` alone where given)."""
+    """The product's inputs on the GPU, and its reference (of the columns `cols` alone where given).  kind: make_ids'
+    or the ids themselves."""
     b, K = _b(), sum(split)
-    ids = C.make_ids(tokens * top_k, experts, kind, seed)
+    ids = C.make_ids(tokens * top_k, experts, kind, seed) if isinstance(kind, str) else kind
     xb, perms = C.activations(tokens, K, experts if own_sigma else 1, seed)
     wb = C.weights(experts, N, K, seed)
     w = _stack(wb, perms, split, formats)
@@ -229,6 +230,25 @@ def test_gemm_grouped_kernels(kernel, slots, experts, N, split, formats):
     y = _b().gemm_grouped(a, w, g)
     torch.cuda.synchronize()
     _check_rows(y[:, torch.from_numpy(cols).cuda()], ref, 0.0, (kernel, formats))
+
+
+@pytest.mark.parametrize("formats", [("E3M2", "E4M3"), ("E2M3", "E5M2"), ("E3M2", "E5M2"), ("E2M3", "E4M3")], ids="-".join)
+@pytest.mark.parametrize("first,second", [(1501, 1499), (0, 2999), (1000, 0), (1500, 0), (0, 0), (1, 129)])
+def test_gemm_grouped_last_round(first, second, formats):
+    """256 x 256 tiles with the last round's in quarters: whole rounds with few tiles behind them, tiles for quarters
+    alone or for whole tiles alone, none.  Rows of the two experts; the others of the 3000 are in no group."""
+    slots, N, split, cus = 3000, 5400, (1024, 160, 832), torch.cuda.get_device_properties(0).multi_processor_count
+    if cus == 256:
+        assert R.route(slots, 2, N, split, cus)[0] == "tiled256x256+rest"
+    note(f"gemm grouped last round {first} {second} {formats}")
+    ids = np.full(slots, -1, np.int32)
+    at = np.random.default_rng(first).permutation(slots)
+    ids[at[:first]], ids[at[first:first + second]] = 0, 1
+    cols = np.unique(np.concatenate([np.arange(0, N, 27), np.arange(N - 40, N)]))
+    ids, g, a, w, ref = _grouped(slots, 1, 2, N, split, ids, formats, seed=10, cols=cols)
+    y = _b().gemm_grouped(a, w, g)
+    torch.cuda.synchronize()
+    _check_rows(y[:, torch.from_numpy(cols).cuda()], ref, 0.0, (first, second, formats))
 
 
 def test_gemm_grouped_matches_gemm_alone():
