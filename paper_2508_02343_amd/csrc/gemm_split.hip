@@ -143,13 +143,11 @@ struct Scales {
 // The activation rows that a tile's loads take: every row of its fragments, or the
 // first n ones (the others take the tile's first row in their place).
 struct AllRows {
-  __device__ __forceinline__ int fragment(int j) const { return j; }
-  __device__ __forceinline__ int row(int, int lane) const { return lane & 31; }
+  __device__ __forceinline__ int row(int lane) const { return lane & 31; }
 };
 struct FirstRows {
   int n;  // at least 1, of one fragment
-  __device__ __forceinline__ int fragment(int j) const { return j; }
-  __device__ __forceinline__ int row(int, int lane) const { return (lane & 31) < n ? lane & 31 : 0; }
+  __device__ __forceinline__ int row(int lane) const { return (lane & 31) < n ? lane & 31 : 0; }
 };
 
 template <int G, int TN, int TM, class Rows>
@@ -157,7 +155,7 @@ __device__ __forceinline__ void load_stage(Stage<TN, TM>& b, const Desc& d, int 
 #pragma unroll
   for (int i = 0; i < TN; ++i) b.w[i] = load_frag<G>(d.w, i, h, lane, lane & 31);
 #pragma unroll
-  for (int j = 0; j < TM; ++j) b.x[j] = load_frag<G>(d.x, rows.fragment(j), h, lane, rows.row(j, lane));
+  for (int j = 0; j < TM; ++j) b.x[j] = load_frag<G>(d.x, j, h, lane, rows.row(lane));
 }
 
 template <int TN, int TM, class Rows>
@@ -167,8 +165,8 @@ __device__ __forceinline__ void load_scales(Scales<TN, TM>& s, const Desc& d, in
   for (int i = 0; i < TN; ++i) s.w[i] = __builtin_amdgcn_raw_buffer_load_b32(d.sw, off, i * kRowGroup * kStepBlocks, 0);
 #pragma unroll
   for (int j = 0; j < TM; ++j)
-    s.x[j] = __builtin_amdgcn_raw_buffer_load_b32(d.sx, rows.row(j, lane) * kStepBlocks,
-                                                  rows.fragment(j) * kRowGroup * kStepBlocks, 0);
+    s.x[j] = __builtin_amdgcn_raw_buffer_load_b32(d.sx, rows.row(lane) * kStepBlocks,
+                                                  j * kRowGroup * kStepBlocks, 0);
 }
 
 // Lane 32 g + r feeds the scale of block 2 h + g of its row, h the 64-channel
