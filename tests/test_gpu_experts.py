@@ -359,6 +359,54 @@ def test_gemv_long(rows, split):
     _check_gemv(y, ref, tol, 0.0, (rows, split))
 
 
+# ---- offsets beyond 32 bits ----
+
+
+def test_offsets_beyond_32_bits():
+    """Weights behind 4 GiB of other experts', rows of x and of the results further apart than 4 GiB in all."""
+    note("offsets beyond 32 bits")
+    b, E, N, split = _b(), 5, 33000, (0, 0, 32768)
+    K, last = sum(split), E - 1
+    cols = np.unique(np.concatenate([np.arange(0, N, 2111), np.arange(N - 3, N)]))
+    perm = np.random.default_rng(71).permutation(K).astype(np.int32)
+    p = to_dev_perm(perm)
+    w = b.MXStack.empty(E, N, K, split)
+    assert last * (w.q8.nbytes // E) > 1 << 32
+    wb = np.zeros((E, len(cols), K), np.uint16)
+    for e in (0, last):
+        torch.manual_seed(e)
+        we = (torch.randn(N, K, device="cuda") * 0.02).bfloat16()
+        b.quantize_weight(we, p, split, out=w[e])
+        wb[e] = we[torch.from_numpy(cols).cuda()].cpu().view(torch.int16).numpy().view(np.uint16)
+        del we
+    at = torch.from_numpy(cols).cuda()
+    for tokens in (3, 5, 700):  # the K-splitting kernel, 256 x 128 and 256 x 256 tiles
+        ids = np.random.default_rng(tokens).choice(np.array([0, last, -1], np.int32), tokens)
+        ids[-1] = last
+        xb, _ = C.activations(tokens, K, 1, seed=tokens)
+        apart = -(-(1 << 32) // (2 * (tokens - 1))) // 64 * 64 + 64  # elements from row to row
+        apart = max(apart, K + 64)
+        x = torch.empty(tokens * apart, dtype=torch.bfloat16, device="cuda").view(tokens, apart)[:, :K]
+        x.copy_(to_dev_bf16(xb))
+        yb = torch.empty(tokens * max(apart, N + 64), dtype=torch.bfloat16, device="cuda").view(tokens, -1)[:, :N]
+        assert (tokens - 1) * x.stride(0) * 2 > 1 << 32 and (tokens - 1) * yb.stride(0) * 2 > 1 << 32
+        yb.fill_(7.0)
+        d = _dev_ids(ids)
+        g = b.group_rows(d, E)
+        b.gemm_grouped(b.quantize_act_grouped(x, g, p, split), w, g, y=yb)
+        torch.cuda.synchronize()
+        _check_rows(yb[:, at], C.grouped_product(xb, ids, 1, [perm], wb, split, DEFAULT), 7.0, (tokens, "gemm"))
+        if tokens <= 16:
+            yb.fill_(7.0)
+            b.gemv(x, w, p, ids=d, y=yb)
+            torch.cuda.synchronize()
+            ref, tol = C.gemv_product(xb, ids, 1, [perm], wb, split, DEFAULT)
+            _check_gemv(yb[:, at], ref, tol, 7.0, (tokens, "gemv"))
+        del x, yb
+    del w
+    torch.cuda.empty_cache()
+
+
 # ---- used together ----
 
 
