@@ -251,6 +251,39 @@ def test_gemm_grouped_last_round(first, second, formats):
     _check_rows(y[:, torch.from_numpy(cols).cuda()], ref, 0.0, (first, second, formats))
 
 
+def test_last_round_captured_and_replayed():
+    """One captured graph, ids that leave the quarters some, all or none of the tiles in turn."""
+    note("last round captured")
+    b, slots, N, split = _b(), 3000, 5400, (1024, 160, 832)
+    K = sum(split)
+    xb, perms = C.activations(slots, K, 1, seed=12)
+    w, x, p = _stack(C.weights(2, N, K, seed=12), perms, split), to_dev_bf16(xb), to_dev_perm(perms[0])
+    ids = torch.zeros(slots, dtype=torch.int32, device="cuda")
+    g, a = b.RowGroups.empty(slots, 2), b.MXTensor.empty(b.RowGroups.empty(slots, 2).capacity, K, split)
+    y = torch.zeros(slots, N, dtype=torch.bfloat16, device="cuda")
+
+    def chain(y):
+        b.group_rows(ids, 2, out=g)
+        b.quantize_act_grouped(x, g, p, split, out=a)
+        b.gemm_grouped(a, w, g, y=y)
+
+    chain(y)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        chain(y)
+    for live in (3000, 1000, 1500, 0, 2990, 130):
+        ids.fill_(-1)
+        ids[:live] = torch.arange(live, device="cuda", dtype=torch.int32) % 2
+        for t in (y, eager := torch.empty_like(y)):
+            t.fill_(7.0)
+        graph.replay()
+        chain(eager)
+        torch.cuda.synchronize()
+        assert torch.equal(y, eager), live
+        assert bool((y[live:] == 7.0).all()) and (live == 0 or not bool((y[:live] == 7.0).all(1).any())), live
+
+
 def test_gemm_grouped_matches_gemm_alone():
     """One expert with every row is mm_gemm, up to the order of the fp32 sums."""
     note("gemm grouped against gemm")
