@@ -64,7 +64,7 @@ def gemm_bytes(M: int, N: int, K: int, split) -> int:
 
 # sources the GEMM kernels above ("tiled") and up to that many rows ("direct") are
 # compiled from (a committed counter summary is used only while they are unchanged)
-GEMM_SOURCES = {"tiled": ("gemm_tiled.hip", "gemm_common.hpp", "grouped.hpp", "mx_device.hpp", "kernels.hpp"),
+GEMM_SOURCES = {"tiled": ("gemm_tiled.hip", "tile_order.hpp", "gemm_common.hpp", "grouped.hpp", "mx_device.hpp", "kernels.hpp"),
                 "direct": ("gemm_direct.hip", "gemm_split.hip", "gemm_route.hpp", "gemm_common.hpp", "grouped.hpp",
                            "mx_device.hpp", "kernels.hpp")}
 CALIB_BYTES = 256 << 20  # plain copy used to calibrate the FETCH_SIZE / WRITE_SIZE counters

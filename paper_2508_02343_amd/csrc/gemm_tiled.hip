@@ -70,6 +70,7 @@
 
 #include "gemm_common.hpp"
 #include "grouped.hpp"
+#include "tile_order.hpp"
 
 namespace mm {
 
@@ -674,11 +675,6 @@ struct Grouped {
 struct Rest {
   Grouped of;
 };
-// How many of nt tiles are not the Rest's.
-__device__ __forceinline__ int in_rounds(int nt, int whole) {
-  const int rest = whole ? nt % whole : 0;
-  return 2 * rest <= whole ? nt - rest : nt;
-}
 
 // Args: Plain, Grouped or Rest (the grid covers as many tiles as there may be; the
 // workgroups past those that there are end at once, so that the tiles go evenly to
@@ -692,40 +688,18 @@ __global__ __launch_bounds__((Tile<BN, BM>::kThreads), (Tile<BN, BM>::kPerCu)) v
     if constexpr (kRest) return args.of;
     else return args;
   }();
-  const int tiles_n = shape.tiles_n;
-  int tiles_m, nt, t_first = 0;
+  GridTile at;
   if constexpr (kGrouped) {
-    tiles_m = *shape.count;
-    tiles_m = tiles_m < shape.tiles_m ? tiles_m : shape.tiles_m;
-    nt = in_rounds(tiles_n * tiles_m, shape.whole);
-    if constexpr (kRest) {
-      t_first = nt;
-      nt = 4 * (tiles_n * tiles_m - nt);
-    }
-    if ((int)blockIdx.x >= nt) return;  // uniform
+    at = grouped_tile(blockIdx.x, shape.tiles_n, shape.tiles_m, *shape.count, shape.whole, kRest);
+    if (!at.live) return;  // uniform
     a = shape.g.g;
   } else {
-    tiles_m = args.tiles_m;
-    nt = tiles_n * tiles_m;
+    at = tile_in_order(tile_of_xcd(blockIdx.x, shape.tiles_n * shape.tiles_m), 0, shape.tiles_n, shape.tiles_m);
     a = args.g;
   }
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
-  constexpr int kGroupN = 4;  // weight tiles that share an XCD's L2 at a time
 
-  // workgroup -> tile: consecutive tiles per XCD (workgroups are dealt to the
-  // 8 XCDs round-robin), then groups of kGroupN weight tiles, activation
-  // tiles fastest inside a group
-  const int wg = blockIdx.x;
-  const int xcd = wg & 7, kq = wg >> 3;
-  const int per_x = nt >> 3, extra = nt & 7;
-  int t = xcd * per_x + (xcd < extra ? xcd : extra) + kq;
-  const int part = t & 3;  // kRest: quarter of a tile
-  if constexpr (kRest) t = t_first + (t >> 2);
-  const int grp = t / (kGroupN * tiles_m);
-  const int within = t - grp * kGroupN * tiles_m;
-  const int gn = tiles_n - grp * kGroupN < kGroupN ? tiles_n - grp * kGroupN : kGroupN;
-  const int tn = grp * kGroupN + within % gn;
-  const int tm = within / gn;
+  const int tn = at.tn, tm = at.tm, part = at.part;
   const int64_t n0 = kRest ? (int64_t)tn * (2 * BN) + (part & 1) * BN : (int64_t)tn * BN;
   int64_t m0 = (int64_t)tm * BM;
   int64_t x_rows = a.x.rp;  // activation rows that may be read
