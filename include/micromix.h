@@ -376,7 +376,9 @@ mm_status mm_gemm_grouped(const mm_mx_tensor* a, const mm_mx_tensor* w, const mm
                           int64_t ldy, void* stream);
 
 /*
- * Device workspace mm_gemv needs for `rows` rows (1 .. 16).  Host-only arithmetic.
+ * Device workspace that mm_gemv takes for `rows` rows (1 .. 16) of one weight, enough
+ * for any experts too.  With ids and at least as many experts as rows mm_gemv takes
+ * none.  Host-only arithmetic.
  * Errors: MM_ERR_NULL (bytes is NULL), MM_ERR_SHAPE, MM_ERR_SPLIT.
  */
 mm_status mm_gemv_workspace_size(int64_t rows, int64_t K, mm_split split, int64_t* bytes);
@@ -397,9 +399,9 @@ mm_status mm_gemv_workspace_size(int64_t rows, int64_t K, mm_split split, int64_
  *   ids         device, int32 [rows], 4-byte aligned, any values; NULL: every row
  *               takes the first weight.
  *   workspace   device, caller-owned, 16-byte aligned, at least
- *               mm_gemv_workspace_size() bytes (NULL where that is 0); contents on
- *               entry ignored, on exit unspecified.  Calls that overlap in time must
- *               not share it.
+ *               mm_gemv_workspace_size() bytes (NULL where that is 0, or with ids
+ *               and rows <= experts); contents on entry ignored, on exit unspecified.
+ *               Calls that overlap in time must not share it.
  *   y_bf16      device, bf16 [rows, N], row stride ldy elements (ldy >= N, ldy % 8 ==
  *               0, 16-byte aligned).
  * Errors: MM_ERR_NULL, MM_ERR_SHAPE, MM_ERR_SPLIT, MM_ERR_ALIGN, MM_ERR_FORMAT,

@@ -566,7 +566,8 @@ def _gemv_workspace(rows: int, K: int, split: tuple) -> int:
 
 
 def gemv_workspace_size(rows: int, K: int, split) -> int:
-    """mm_gemv_workspace_size: device bytes mm_gemv needs."""
+    """mm_gemv_workspace_size: device bytes that suffice for mm_gemv (none with ids and at
+    least as many experts as rows)."""
     return _gemv_workspace(int(rows), int(K), tuple(map(int, split)))
 
 
@@ -598,7 +599,7 @@ def gemv(x: torch.Tensor, w: MXTensor | MXStack, perm: torch.Tensor, ids: torch.
         if not workspace.is_contiguous() or workspace.get_device() != index:
             raise ValueError("workspace must be contiguous and on x's device")
         p_ws, n_ws = workspace.data_ptr(), workspace.nbytes
-    else:
+    elif ids is None or rows > experts:
         n_ws = gemv_workspace_size(rows, K, w.split) if type(w.split) is not tuple else _gemv_workspace(rows, K, w.split)
         if n_ws:
             with _new_on(stream):

@@ -9,6 +9,7 @@
 
 #include "../../include/micromix.h"
 #include "gemm_route.hpp"
+#include "gemv_route.hpp"
 #include "grouped.hpp"
 #include "grouped_route.hpp"
 #include "kernels.hpp"
@@ -17,6 +18,7 @@ namespace {
 
 constexpr int64_t kMaxQuantK = 32768;  // one row of bf16 must fit the LDS budget
 constexpr int64_t kMaxRows = (int64_t)1 << 31;
+static_assert(mm::kGemvMaxK == kMaxQuantK, "mm_gemv's x is as long as the quantisers'");
 // Calibration workspace: the workgroup maxima (nchunks * tiles <= 256 words)
 // and the per-block group counts (2 * K / 256 <= 256 words), then fp64
 // partial sums and means, then int32 per-slice rank counts.
@@ -565,7 +567,7 @@ mm_status mm_gemv_workspace_size(int64_t rows, int64_t K, mm_split split, int64_
   st = check_shape(rows, K, split, who);
   if (st != MM_OK) return st;
   if (K > kMaxQuantK) return fail(MM_ERR_SHAPE, "%s: K=%lld exceeds %lld", who, (long long)K, (long long)kMaxQuantK);
-  *bytes = mm::gemv_workspace_bytes(rows, K, layout(rows, split).steps);
+  *bytes = mm::gemv_workspace_bytes({rows, K, 0, 0, 0}, layout(rows, split).steps);  // (of one weight: the most)
   return MM_OK;
 }
 
@@ -593,7 +595,7 @@ mm_status mm_gemv(const void* x_bf16, int64_t ldx, int64_t rows, int64_t top_k, 
   st = check_result(w, y_bf16, ldy, who);
   if (st != MM_OK) return st;
   const Layout l = layout(w->rows, w->split);
-  const int64_t need = mm::gemv_workspace_bytes(rows, w->K, l.steps);
+  const int64_t need = mm::gemv_workspace_bytes({rows, w->K, w->rows, ids ? experts : 0, 0}, l.steps);
   if (need > 0 && !workspace) return fail(MM_ERR_NULL, "%s: workspace is NULL", who);
   if (workspace_bytes < need)
     return fail(MM_ERR_WORKSPACE, "%s: workspace of %lld bytes, %lld needed", who, (long long)workspace_bytes, (long long)need);

@@ -326,14 +326,17 @@ __global__ __launch_bounds__(64 * kWaves, 4) void gemv_kernel(GemvArgs a, const 
   store_four(a, x.out, n0 + 16 * wave + 4 * q, s);
 }
 
+// What a launch is asked: the plan is the rule's (gemv_route.hpp).
+static GemvSizes sizes_of(const GemvArgs& a, const Device& dev) {
+  return GemvSizes{a.rows, a.K, a.w.rows, a.ids ? a.experts : 0, dev.cus};
+}
+
 template <int FS, int TN, int W>
-static hipError_t launch_gemv_strip(const GemvArgs& a, const Device& dev, hipStream_t stream) {
+static hipError_t launch_gemv_strip(const GemvArgs& a, bool in_lds, const Device& dev, hipStream_t stream) {
   int w[3];
   share_waves(a.steps, kByteCost, W, w);
   const dim3 grid((unsigned)((a.w.rows + 16 * TN - 1) / (16 * TN)), a.ids ? a.rows : 1);
-  // (with experts LDS holds one row; rows that must share experts, as there are fewer,
-  // share their weights' loads only from the workspace)
-  if (gemv_in_lds(a.rows, a.K) || (a.ids && a.rows <= a.experts && gemv_in_lds(1, a.K))) {
+  if (in_lds) {
     static DeviceOnce once;
     hipError_t e = allow_lds(once, dev, reinterpret_cast<const void*>(gemv_kernel<FS, TN, W, true>), (int)kGemvMaxLds);
     if (e != hipSuccess) return e;
@@ -350,20 +353,15 @@ static hipError_t launch_gemv_strip(const GemvArgs& a, const Device& dev, hipStr
   return hipGetLastError();
 }
 
-// Strips and wavefronts.  One strip of 16 rows and sixteen wavefronts for every CU as
-// long as there are no more of them (us, 1 row, K x N: 4096 x 4096 5.6 against 6.3
-// with eight and 6.4 with 32 rows, 14336 x 4096 10.9 / 12.4 / 13.6); above, strips of
-// 32 rows (whole records of the layout), with fewer wavefronts the more strips
-// share a CU: four beyond two strips per CU (two experts of 14336 x 4096 in E2M1 14.4,
-// with eight 16.3), eight beyond one (14336 rows of K 4096 10.5, with four 11.1, with
-// sixteen 11.9), else sixteen (two experts of 4096 x 14336 16.8, with eight 18.7).
 template <int FS>
 static hipError_t launch_gemv_fs(const GemvArgs& a, const Device& dev, hipStream_t stream) {
-  const int64_t units = a.ids ? a.rows : 1, strips = units * ((a.w.rows + 31) / 32);
-  if (units * ((a.w.rows + 15) / 16) <= dev.cus) return launch_gemv_strip<FS, 1, 16>(a, dev, stream);
-  if (strips <= dev.cus) return launch_gemv_strip<FS, 2, 16>(a, dev, stream);
-  if (strips <= 2 * dev.cus) return launch_gemv_strip<FS, 2, 8>(a, dev, stream);
-  return launch_gemv_strip<FS, 2, 4>(a, dev, stream);
+  const GemvPlan p = gemv_plan(sizes_of(a, dev));
+  if (p.tn == 1) return launch_gemv_strip<FS, 1, 16>(a, p.in_lds, dev, stream);
+  switch (p.waves) {
+    case 16: return launch_gemv_strip<FS, 2, 16>(a, p.in_lds, dev, stream);
+    case 8: return launch_gemv_strip<FS, 2, 8>(a, p.in_lds, dev, stream);
+    default: return launch_gemv_strip<FS, 2, 4>(a, p.in_lds, dev, stream);
+  }
 }
 
 // The format set is a compile-time choice of conversions: one kernel per set.

@@ -2,6 +2,7 @@
 // ordered by expert, and of the matrix-vector kernel.
 #pragma once
 
+#include "gemv_route.hpp"
 #include "kernels.hpp"
 
 namespace mm {
@@ -126,10 +127,6 @@ hipError_t launch_gemm_tiled_grouped(const GemmGroupedArgs& a, int bn, int bm, b
 // 64 x 32 (weights of at least 64 padded rows), else 32 x 32
 hipError_t launch_gemm_split_grouped(const GemmGroupedArgs& a, bool wide, const Device& dev, hipStream_t stream);
 
-// At most this many rows in a call of the matrix-vector kernel.
-constexpr int kGemvMaxRows = 16;
-constexpr int64_t kGemvMaxN = (int64_t)1 << 28;  // (a launch has fewer than 2^32 threads)
-
 struct GemvArgs {
   const uint16_t* x;
   int64_t ldx;
@@ -146,18 +143,8 @@ struct GemvArgs {
   uint16_t* y;
   int64_t ldy;
   int fs;
-  void* workspace;  // gemv_workspace_bytes(rows, K, steps)
+  void* workspace;  // gemv_workspace_bytes
 };
-// LDS of a workgroup of `waves` wavefronts that holds `rows` rows of x: the rows, and
-// 64 words of each per wavefront.  Up to kGemvMaxLds with the most wavefronts, x goes
-// that way; beside it the workgroup has 32 KB of sums.
-constexpr int kGemvMaxWaves = 16;
-constexpr int64_t kGemvMaxLds = 110 * 1024;
-inline int64_t gemv_lds_bytes(int64_t rows, int64_t K, int waves) { return rows * (2 * K + 1024 * (int64_t)waves); }
-inline bool gemv_in_lds(int64_t rows, int64_t K) { return gemv_lds_bytes(rows, K, kGemvMaxWaves) <= kGemvMaxLds; }
-inline int64_t gemv_workspace_bytes(int64_t rows, int64_t K, const int* steps) {
-  return gemv_in_lds(rows, K) ? 0 : rows * 256 * ((int64_t)steps[0] + steps[1] + steps[2]);
-}
 hipError_t launch_gemv(const GemvArgs& a, const Device& dev, hipStream_t stream);
 
 }  // namespace mm
