@@ -10,11 +10,11 @@
 // agree, so a lane takes a packed block whole: lane 16 q + r holds block q of row
 // r of a layout step, and product i of the step its elements 8 i .. 8 i + 7.
 //
-// x has to be in that order as well, gathered by sigma.  Where a workgroup's rows of x
-// fit its LDS (one row with experts; rows x K up to a few ten thousand values), it
-// takes them there as they are, behind its first weight loads, and every wavefront
-// gathers the words of a batch of steps for itself.  More: a launch of its own puts
-// all of x in order in the workspace, from where the lanes load their words (L2).
+// x has to be in that order as well, gathered by sigma.  Few rows (gemv_route.hpp) a
+// workgroup takes into LDS as they are (with experts one row), behind its first
+// weight loads, and every wavefront gathers the words of a batch of steps for itself.
+// More: a launch of its own puts all of x in order in the workspace, from where the
+// lanes load their words (L2).
 //
 // Measured (us; K x N, split 75 / 18.75 / 6.25 % where not said, weights from HBM): 1
 // row, 4096 x 4096 in (2048, 1024, 1024) 5.7 (2.1 TB/s; quantiser and GEMM 3.7 + 4.4),

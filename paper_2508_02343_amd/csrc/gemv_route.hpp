@@ -24,11 +24,23 @@ struct GemvSizes {
   int cus;
 };
 
-// From LDS (one launch) go rows that fit it with the most wavefronts, and rows that each
-// have an expert of their own to find (at least as many experts as rows: a workgroup
-// then holds one row).  The others from the workspace, where a launch in front puts
-// them in order.  (With experts LDS holds one row; rows that must share experts, as there
-// are fewer, share their weights' loads only from the workspace.)
+// With experts a workgroup's LDS holds one row, so every row loads its expert's weight for
+// itself; from the workspace, where a launch in front puts x in order, rows that share an
+// expert are columns of one product and share its loads.  Without ids all rows share the
+// one weight either way.  From LDS (one launch) go rows few enough to fit it all together,
+// and rows with at least as many experts as rows; the others from the workspace.
+//
+// Measured with experts chosen at random (us, LDS / workspace; 75 / 18.75 / 6.25 %, weights
+// from HBM), where the rule takes LDS: 2 rows on 2 experts of 2048 x 4096 (K x N) 5.5 / 8.3, on 8
+// of 4096 x 14336 17.2 / 21.0; 4 rows on 64 experts of 4096 x 4096 12.1 / 14.6; 16 on 64 of 2048
+// x 1024 8.2 / 12.1, of 4096 x 14336 90.8 / 95.9; 8 on 8 of 4096 x 4096 16.2 / 19.2, of 4096 x 14336
+// 46.3 / 43.1; few rows that fit on fewer experts: 4 on 2 of 2048 x 1024 4.7 / 7.2, of 4096 x 4096
+// 9.9 / 10.7, but of 4096 x 14336 26.0 / 19.4.  Where it takes the workspace: 16 rows on 2 of 4096
+// x 14336 81.9 / 24.3, on 8 of 4096 x 4096 28.0 / 24.0, 8 on 2 of 14336 x 4096 39.2 / 32.0, but
+// small weights stay in the caches and the second launch is not worth it: 16 on 8 of 2048 x
+// 1024 6.6 / 10.4, 8 on 2 of 4096 x 4096 13.2 / 13.6.  Over 336 such sizes the choice takes 6 % more
+// than the better one in the mean, 1.76 times at worst; LDS only up to as many rows as experts
+// would take 10 %, LDS always 10 % and 5.1 times at worst, the workspace always 23 %.
 inline bool gemv_in_lds(const GemvSizes& a) {
   return gemv_lds_bytes(a.rows, a.K, kGemvMaxWaves) <= kGemvMaxLds || (a.experts > 0 && a.rows <= a.experts);
 }
