@@ -471,15 +471,16 @@ __device__ __forceinline__ void shift_scales(Ops<BN, BM>& o, int shift) {
 // between two stages' MFMAs nothing is left to issue (with the cursor, the
 // addresses, the scale shifts and the waits between the stages, the matrix
 // cores idled for 200-400 cycles of each):
-//  - the first three quarters (kR): the loads that refill stage q's slot and
-//    the reads of stage q+1 (for the group's last stage they are of no use,
-//    harmlessly, and the next group reads its first stage again);
+//  - the first three quarters (kR; half of a stage of 8 or 4 MFMAs): the loads
+//    that refill stage q's slot and the reads of stage q+1 (for the group's last
+//    stage they are of no use, harmlessly, and the next group reads its first
+//    stage again);
 //  - then the cursor's and the addresses' step to the next stage;
-//  - three MFMAs before the end the synchronisation that the next stage
-//    needs: this wavefront's reads of stage q+1 are done (its slot is
-//    refilled next), its loads of stage q+2 have landed (every stage issues
-//    kLoads, and the NS - 2 stages after q+2 may still be in flight), and so
-//    for everyone at the barrier;
+//  - three MFMAs before the end (kS; with the last one in a stage of 4) the
+//    synchronisation that the next stage needs: this wavefront's reads of stage
+//    q+1 are done (its slot is refilled next), its loads of stage q+2 have landed
+//    (every stage issues kLoads, and the NS - 2 stages after q+2 may still be in
+//    flight), and so for everyone at the barrier;
 //  - behind the last two, stage q+1's scale shifts.
 template <int G, int FS, int T, int BN, int BM>
 __device__ __forceinline__ void mfma_block(const Ctx<BN, BM>& c, Acc<BN, BM>& acc, const Ops<BN, BM>& o,
@@ -488,8 +489,9 @@ __device__ __forceinline__ void mfma_block(const Ctx<BN, BM>& c, Acc<BN, BM>& ac
   constexpr int TN = Ti::TN, TM = Ti::TM, F = Ti::F, NS = Ti::kSlots;
   constexpr int kPer = TN * TM;
   constexpr int kM = stage_slices(G) * kPer;
-  constexpr int kR = kM == 4 ? 2 : (kM == 8 ? 4 : kM * 3 / 4), kS = kR + 1;
+  constexpr int kR = kM == 4 ? 2 : (kM == 8 ? 4 : kM * 3 / 4), kS = kM == 4 ? 3 : kM - 3;
   constexpr int kSh = kM == 4 ? 3 : kM - 2;  // the first half of the scale shifts: behind the wait
+  static_assert(kS > kR && kS <= kSh, "the waits follow the reads and loads, the scale shifts the waits");
   if constexpr (T < kM) {
     constexpr int fmt = group_fmt(G, FS);
     constexpr int KK = T / kPer, i = (T % kPer) / TM, j = T % TM;
