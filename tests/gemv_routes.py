@@ -40,3 +40,26 @@ def plan(rows: int, N: int, split, experts: int = 0, cus: int = 256) -> tuple[in
     line = " ".join(str(v) for v in (rows, sum(split), N, experts, cus, *steps))
     out = subprocess.run([_program()], input=line, check=True, capture_output=True, text=True).stdout.split()
     return int(out[0]), int(out[1]), out[2] == "1", int(out[3])
+
+
+# One case per compiled kernel: (strips, wavefronts, x from LDS), rows, experts (0: one weight), N.  The splits below
+# take every case to several batches of steps, with the last one not full.
+CASES = [
+    ((1, 16, True), 1, 0, 301),
+    ((1, 16, False), 9, 0, 301),
+    ((2, 16, True), 1, 0, 6001),
+    ((2, 16, False), 9, 0, 5003),
+    ((2, 8, True), 2, 0, 9001),
+    ((2, 8, False), 9, 0, 8301),
+    ((2, 4, True), 1, 0, 16999),
+    ((2, 4, False), 9, 0, 16411),
+    ((1, 16, True), 6, 8, 301),
+    ((1, 16, False), 9, 4, 301),
+    ((2, 16, True), 6, 8, 1201),
+    ((2, 16, False), 9, 4, 801),
+    ((2, 8, True), 6, 8, 2303),
+    ((2, 8, False), 9, 4, 1501),
+    ((2, 4, True), 6, 8, 4001),
+    ((2, 4, False), 9, 4, 2501),
+]
+SPLITS = [(1408, 544, 480), (1440, 0, 0), (0, 1440, 0), (0, 0, 1440)]

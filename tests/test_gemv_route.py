@@ -5,7 +5,7 @@ import ctypes
 import pytest
 
 from paper_2508_02343_amd import binding as b
-from tests.gemv_routes import plan
+from tests.gemv_routes import CASES, SPLITS, plan
 
 FAKE = 0x10000  # 16-byte aligned, never dereferenced: validation fails first
 SPLIT, K = (64, 32, 32), 128
@@ -50,3 +50,9 @@ def test_one_rule_for_launch_and_workspace(split):
             assert (need == 0) == in_lds
             assert need in (0, _size(rows, split))
             assert in_lds or experts < rows  # (with an expert for every row never)
+
+
+@pytest.mark.parametrize("form,rows,experts,N", CASES, ids=str)
+def test_every_form_is_reached(form, rows, experts, N):
+    for split in SPLITS:
+        assert plan(rows, N, split, experts)[:3] == form

@@ -71,3 +71,54 @@ def test_rows_with_experts_of_their_own_take_no_workspace(rows, top_k, experts):
     assert torch.cuda.memory_stats()["allocation.all.allocated"] == before
     torch.cuda.synchronize()
     _check(y, ref, tol, 7.0, "binding")
+
+
+@pytest.mark.parametrize("formats", [("E3M2", "E4M3"), ("E2M3", "E5M2"), ("E3M2", "E5M2"), ("E2M3", "E4M3")], ids="-".join)
+@pytest.mark.parametrize("split", R.SPLITS, ids=str)
+@pytest.mark.parametrize("form,rows,experts,N", R.CASES, ids=str)
+def test_every_form(form, rows, experts, N, split, formats):
+    """Every compiled kernel with every format set, three groups and each alone, widths that are no multiple of a strip;
+    x with a stride, guard columns beside y."""
+    assert R.plan(rows, N, split, experts, _cus())[:3] == form
+    note(f"gemv {form} rows={rows} E={experts} N={N} {split} {formats}")
+    b, K, E = _b(), sum(split), max(experts, 1)
+    xb, perms = C.activations(rows, K, E, seed=rows + N)
+    # columns of the result to compare: some of every strip's 16-row halves, and the last ones
+    cols = np.unique(np.concatenate([np.arange(0, N, max(1, N // 60)), np.arange(N - min(N, 40), N)]))
+    at = torch.from_numpy(cols).cuda()
+    w = b.MXStack.empty(E, N, K, split, formats=formats)
+    wb = np.zeros((E, len(cols), K), np.uint16)
+    for e in range(E):
+        g = torch.Generator("cuda").manual_seed(1000 * N + e)
+        we = (torch.randn(N, K, generator=g, device="cuda") * 0.02).bfloat16()
+        b.quantize_weight(we, to_dev_perm(perms[e]), split, out=w[e])
+        wb[e] = we[at].cpu().view(torch.int16).numpy().view(np.uint16)
+    ids = C.make_ids(rows, experts, "even", seed=N) if experts else None
+    if experts:
+        ids[1] = -1
+    wide_x = torch.full((rows, K + 8), float("nan"), dtype=torch.bfloat16, device="cuda")
+    wide_x[:, :K] = to_dev_bf16(xb)
+    wide = torch.full((rows, (N + 7) // 8 * 8 + 8), 7.0, dtype=torch.bfloat16, device="cuda")
+    b.gemv(wide_x[:, :K], w if experts else w[0], to_dev_perm(perms if experts else perms[0]),
+           ids=None if ids is None else torch.from_numpy(ids).cuda(), y=wide[:, :N])
+    torch.cuda.synchronize()
+    ref, tol = C.gemv_product(xb, ids, 1, perms, wb, split, formats)
+    _check(wide[:, at], ref, tol, 7.0, (form, split, formats))
+    assert bool((wide[:, N:] == 7.0).all()), "columns behind the result"
+
+
+@pytest.mark.parametrize("experts", [257, 1024])
+def test_many_experts(experts):
+    """Rows of the first and the last of many experts, and of those around 256."""
+    note(f"gemv {experts} experts")
+    b, N, split = _b(), 40, (96, 64, 64)
+    K = sum(split)
+    ids = np.array([0, experts - 1, 255, 256, 1, experts, -1, experts - 1, experts - 2, 128], np.int32)
+    xb, perms = C.activations(len(ids), K, experts, seed=experts)
+    wb = C.weights(experts, N, K, seed=experts)
+    w = _stack(wb, perms, split)
+    y = torch.full((len(ids), N), 7.0, dtype=torch.bfloat16, device="cuda")
+    b.gemv(to_dev_bf16(xb), w, to_dev_perm(perms), ids=torch.from_numpy(ids).cuda(), y=y)
+    torch.cuda.synchronize()
+    ref, tol = C.gemv_product(xb, ids, 1, perms, wb, split, DEFAULT)
+    _check(y, ref, tol, 7.0, experts)
