@@ -599,7 +599,7 @@ def gemv(x: torch.Tensor, w: MXTensor | MXStack, perm: torch.Tensor, ids: torch.
         if not workspace.is_contiguous() or workspace.get_device() != index:
             raise ValueError("workspace must be contiguous and on x's device")
         p_ws, n_ws = workspace.data_ptr(), workspace.nbytes
-    elif ids is None or rows > experts:
+    elif ids is None or not 0 < rows <= experts:
         n_ws = gemv_workspace_size(rows, K, w.split) if type(w.split) is not tuple else _gemv_workspace(rows, K, w.split)
         if n_ws:
             with _new_on(stream):

@@ -122,3 +122,15 @@ def test_many_experts(experts):
     torch.cuda.synchronize()
     ref, tol = C.gemv_product(xb, ids, 1, perms, wb, split, DEFAULT)
     _check(y, ref, tol, 7.0, experts)
+
+
+@pytest.mark.parametrize("experts", [0, 8])
+def test_no_rows_are_refused_as_a_shape(experts):
+    b, split = _b(), (64, 32, 32)
+    w = b.MXStack.empty(max(experts, 1), 40, 128, split)
+    x = torch.zeros(4, 128, dtype=torch.bfloat16, device="cuda")
+    p = torch.arange(128, dtype=torch.int32, device="cuda")
+    ids = torch.zeros(0, dtype=torch.int32, device="cuda") if experts else None
+    with pytest.raises(b.MMError, match="MM_ERR_SHAPE"):
+        b.gemv(x[:0], w if experts else w[0], p, ids=ids)
+    assert b.gemv(x[:1], w[0], p).shape == (1, 40)
