@@ -16,14 +16,15 @@
 // More: a launch of its own puts all of x in order in the workspace, from where the
 // lanes load their words (L2).
 //
-// Measured (us; K x N, split 75 / 18.75 / 6.25 % where not said, weights from HBM): 1
-// row, 4096 x 4096 in (2048, 1024, 1024) 5.7 (2.1 TB/s; quantiser and GEMM 3.7 + 4.4),
-// 14336 x 4096 10.9 (3.4 TB/s), 4096 x 14336 10.5; two experts of 4096 x 14336 in E2M1
-// 14.4 (4.3 TB/s); 8 rows, 27648 x 5120 28.5 (3.0 TB/s), where the words of x from L2, as
-// many bytes as the weight's, bound it.  Tried: every workgroup putting all of x in
-// order before it begins (6.3, 12.7 and 11.3 on the first three), a persistent
-// workgroup with two batches in turn (7.8, 18.1: the registers of the second batch
-// leave a SIMD two wavefronts), one step at a time (12.4 with the extra launch).
+// Measured (us, as graph replays; K x N, split 75 / 18.75 / 6.25 % where not said, weights
+// from HBM): 1 row, 4096 x 4096 in (2048, 1024, 1024) 5.6 (2.2 TB/s; quantiser and GEMM
+// 3.7 + 4.4), 14336 x 4096 10.6 (3.4 TB/s), 4096 x 14336 10.4 (3.4); two experts of 4096 x
+// 14336 in E2M1 15.0 (4.2 TB/s); 16 rows with an expert each of 2048 x 1024 7.8 (2.7 TB/s);
+// 8 rows, 27648 x 5120 28.9 (3.0 TB/s), where the words of x from L2, as many bytes as the
+// weight's, bound it.  Tried: every workgroup putting all of x in order before it begins
+// (6.3, 12.7 and 11.3 on the first three), a persistent workgroup with two batches in
+// turn (7.8, 18.1: the registers of the second batch leave a SIMD two wavefronts), one
+// step at a time (12.4 with the extra launch).
 #include "gemm_common.hpp"
 #include "gemm_route.hpp"
 #include "grouped.hpp"

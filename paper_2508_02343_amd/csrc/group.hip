@@ -12,10 +12,10 @@
 // More than kGroupChunk slots: a first launch leaves each workgroup's counts, the
 // second places.
 //
-// Measured (us, as graph replays): 16 slots of 8 experts 6.5, 65536 of 128 11.7 (two
-// launches; 0.05 TB/s of ids and rows).  What it takes is its chain of steps: the
+// Measured (us, as graph replays): 16 slots of 8 experts 5.5, 65536 of 128 9.8 (two
+// launches; 0.06 TB/s of ids and rows).  What it takes is its chain of steps: the
 // ids' load, a ballot per bit, four barriers, the stores.  With 4096 slots per
-// workgroup and the ids read twice instead of kept with their ranks, 21.5.
+// workgroup and the ids read twice instead of kept with their ranks, 21.5 (then 11.7).
 #include "grouped.hpp"
 
 namespace mm {

@@ -12,10 +12,11 @@
 // group, which share cache lines in the packed layout, meet in one L2.  sigma stays
 // in registers until the expert changes.
 //
-// Measured (us): 16 rows of K 4096 4.5; 4096 slots x 4096, two per token, 14.9 (2.9
-// TB/s of rows and codes); 8192 slots x 14336, a sigma per expert, 79 (3.9 TB/s).  A run
-// of consecutive passes to each workgroup took 109 on the last (the lines of half-filled
-// row groups do not last in the L2), without the next pass's loads in flight 111.
+// Measured (us, as graph replays): 16 rows of K 4096 4.3; 4096 slots x 4096, two per
+// token, 14.7 (3.0 TB/s of rows and codes); 8192 slots x 14336, a sigma per expert, 76 (4.0
+// TB/s).  A run of consecutive passes to each workgroup took 109 on the last (the lines
+// of half-filled row groups do not last in the L2), without the next pass's loads in
+// flight 111.
 #include "grouped.hpp"
 #include "quantize_common.hpp"
 
